@@ -331,6 +331,38 @@ int lqer_linear_forward_static(const lqer_layer* layer, const float* X_dev, int6
                                float* Y_dev, int64_t ldy, void* hip_stream);
 
 /*
+ * ---- Between a block's linears ---------------------------------------------------------------------------------------
+ * The calls below are what a served decoder block does between two linear calls: lqer_rmsnorm_mx hands a layer its X_q.
+ * The conventions are those above:
+ * asynchronous on the given stream, no allocation, no host synchronisation, capturable in a HIP graph, the same bits
+ * on every run; argument errors are reported before anything is launched.
+ */
+
+/* Types of the values that these calls read and write. */
+typedef enum { LQER_F32 = 0, LQER_BF16 = 1 } lqer_type;
+
+/*
+ * Root-mean-square norm with the residual's addition, its result as MXINT (Sec. 2.2, block [1,16] of Sec. 4.1):
+ *        h = x + residual,   v = h / sqrt(mean(h^2) + eps) * weight,   codes and exponent bytes of v
+ *   x_dev         [rows][ldx], x_type;  residual_dev [rows][ldr] and h_dev [rows][ldh], both res_type (h_dev may be
+ *                 residual_dev itself); both NULL: h = x, nothing is stored
+ *   weight_dev    [cols], weight_type
+ *   cols          multiple of 16; strides in elements, at least cols
+ *   elem_bits     8 or 6, codes_dev int8 [rows][cols], exps_dev uint8 [rows][cols/16]: what lqer_linear_forward_q takes
+ *   values_dev    NULL, or bf16 [rows][ldv]: the numbers the codes stand for (8 significant bits: exact in bf16), for
+ *                 consumers that take no codes
+ * All pointers 16-byte aligned (exps_dev: any), strides multiples of 16 bytes; LQER_ERR_SHAPE otherwise.  h is the fp32 sum,
+ * rounded once more where res_type is bf16 (v is computed from the fp32 sum); the mean and v are computed in 64
+ * bits, so that a code is that of the exact v but for the rounding of h.  Inputs must be finite, eps >= 0 (a row of zeros with eps = 0 has
+ * codes 0).  rows == 0 or cols == 0 is a no-op.
+ */
+int lqer_rmsnorm_mx(const void* x_dev, int x_type, int64_t rows, int64_t cols, int64_t ldx,
+                    const void* residual_dev, int64_t ldr, void* h_dev, int64_t ldh, int res_type,
+                    const void* weight_dev, int weight_type, float eps,
+                    int elem_bits, int8_t* codes_dev, uint8_t* exps_dev, uint16_t* values_dev, int64_t ldv,
+                    void* hip_stream);
+
+/*
  * Diagnostic, host only (no device call, runs without a GPU): tiles pseudo-random canonical bytes into the device
  * record layouts of Sec. 4.1's formats (4- and 2-bit weights, both exponent forms, ragged sizes, ranks to 256) and back,
  * and compares.  LQER_OK, or LQER_ERR_VALUE at the first difference.  Meant for builds with host sanitizers.

@@ -26,7 +26,8 @@ EXPORTS = ("lqer_status_string", "lqer_quantize_mx", "lqer_build_factors", "lqer
            "lqer_linear_forward", "lqer_linear_forward_q", "lqer_linear_forward_ex", "lqer_linear_forward_requant", "lqer_linear_path",
            "lqer_linear_shared_workspace_bytes", "lqer_linear_forward_shared", "lqer_set_wait_limit",
            "lqer_linear_forward_static", "lqer_layer_import_w", "lqer_layer_weight_bits",
-           "lqer_int_layer_import", "lqer_int_layer_export", "lqer_quantize_int8_token", "lqer_selftest_layouts")
+           "lqer_int_layer_import", "lqer_int_layer_export", "lqer_quantize_int8_token", "lqer_selftest_layouts",
+           "lqer_rmsnorm_mx")
 
 
 class LqerError(RuntimeError):
@@ -113,6 +114,9 @@ def lib() -> C.CDLL:
     L.lqer_linear_path.argtypes = [vp, i64]
     L.lqer_linear_forward_static.restype = i32
     L.lqer_linear_forward_static.argtypes = [vp, vp, i64, i64, vp, i64, vp]
+    f32 = C.c_float
+    L.lqer_rmsnorm_mx.restype = i32
+    L.lqer_rmsnorm_mx.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, i32, vp, i32, f32, i32, vp, vp, vp, i64, vp]
     _lib = L
     return L
 
@@ -403,3 +407,46 @@ def lqer_linear_forward_shared(layers, X, Ys=None, workspace=None):
 
 def lqer_set_wait_limit(polls: int):
     _check(lib().lqer_set_wait_limit(int(polls)), "lqer_set_wait_limit")
+
+
+# ---- between a block's linears ------------------------------------------------------------------------------------------
+def _typed(t, name, *dtypes):
+    """The C ABI sees pointers only: what a tensor holds, and that it is on the GPU, is checked here."""
+    if not t.is_cuda or t.dtype not in dtypes:
+        raise ValueError(f"{name} must be a CUDA tensor of {' or '.join(str(d) for d in dtypes)}")
+    return t
+
+
+def _rows(t, name, cols):
+    """The row stride of a matrix whose last axis is contiguous and has `cols` values."""
+    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
+    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+
+
+def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, elem_bits: int = 8, values: bool = False):
+    """x [rows][cols], residual (or None) of x's shape, weight [cols]: fp32 or bf16 CUDA tensors.  Returns (codes int8, exps uint8,
+    h, values): h is h_out (a new tensor of residual's type unless given; residual itself updates in place), None without a residual;
+    values is the bf16 tensor of what the codes stand for, or None."""
+    import torch
+    f32, bf16 = torch.float32, torch.bfloat16
+    rows, cols = _typed(x, "x", f32, bf16).shape
+    ldx = _rows(x, "x", cols)
+    if _typed(weight, "weight", f32, bf16).shape != (cols,) or not weight.is_contiguous():
+        raise ValueError(f"weight must be [{cols}]")
+    h, ldr, ldh = None, 0, 0
+    if residual is not None:
+        ldr = _rows(_typed(residual, "residual", f32, bf16), "residual", cols)
+        h = torch.empty((rows, cols), dtype=residual.dtype, device=x.device) if h_out is None else _typed(h_out, "h_out", residual.dtype)
+        ldh = _rows(h, "h_out", cols)
+        if residual.shape[0] != rows or h.shape[0] != rows:
+            raise ValueError("residual and h_out must have x's rows")
+    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
+    exps = torch.empty((rows, cols // 16), dtype=torch.uint8, device=x.device)
+    v = torch.empty((rows, cols), dtype=bf16, device=x.device) if values else None
+    _check(lib().lqer_rmsnorm_mx(x.data_ptr(), x.dtype == bf16, rows, cols, ldx,
+                                 None if h is None else residual.data_ptr(), ldr, None if h is None else h.data_ptr(), ldh,
+                                 h is not None and h.dtype == bf16, weight.data_ptr(), weight.dtype == bf16, eps, elem_bits,
+                                 codes.data_ptr(), exps.data_ptr(), None if v is None else v.data_ptr(), cols, _stream()),
+           "lqer_rmsnorm_mx")
+    return codes, exps, h, v

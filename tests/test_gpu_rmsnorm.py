@@ -1,0 +1,117 @@
+"""lqer_rmsnorm_mx against the 64-bit norm and the oracle's quantizer.
+
+Tolerances, derived: h is the fp32 sum x + r, compared bit for bit (and rounded once more to bf16 where the residual is).
+The codes are those of the 64-bit v = h rsqrt(mean h^2 + eps) w of that same fp32 h.  The kernel's v is within a few
+2^-53 of it, so a code differs only where |v| 2^(f - e) is within 2^-40 of a half: with the random data used
+here that has probability 2^-40 a value, so codes, exponent bytes and values are asserted equal."""
+import numpy as np
+import pytest
+
+from oracle import block, mxint
+
+pytestmark = pytest.mark.gpu
+
+
+def _run(rows, cols, xt, rt, wt, bits, pad=0, inplace=False, eps=1e-5, edit=None):
+    import torch
+    from paper_2402_02446_amd import binding
+    t = {"f32": torch.float32, "bf16": torch.bfloat16}
+    g = torch.Generator().manual_seed(rows * 131 + cols)
+    x = torch.randn(rows, cols + pad, generator=g)
+    x[:, ::37] *= 40
+    w = (1 + 0.2 * torch.randn(cols, generator=g)).to(t[wt])
+    r = None if rt is None else (torch.randn(rows, cols + pad, generator=g) * 3).to(t[rt])
+    x = x.to(t[xt])
+    if edit:
+        edit(x, r)
+    h = x[:, :cols].float() if r is None else x[:, :cols].float() + r[:, :cols].float()
+    xd, wd = x.cuda()[:, :cols], w.cuda()
+    rd = None if r is None else r.cuda()[:, :cols]
+    codes, exps, hd, values = binding.lqer_rmsnorm_mx(xd, wd, eps, residual=rd, h_out=rd if inplace else None, elem_bits=bits, values=True)
+    v = block.rmsnorm(h.double().numpy(), w.double().numpy(), float(np.float32(eps)))
+    oc, oe = mxint.mx_quantize(v, bits)
+    assert np.array_equal(exps.cpu().numpy(), oe)
+    assert np.array_equal(codes.cpu().numpy(), oc)
+    assert np.array_equal(values.double().cpu().numpy(), mxint.mx_dequantize(oc, oe, bits))
+    if r is None:
+        assert hd is None
+    else:
+        assert torch.equal(hd.cpu(), h.to(t[rt]))
+        if inplace:
+            assert hd.data_ptr() == rd.data_ptr()
+
+
+@pytest.mark.parametrize("xt", ["f32", "bf16"])
+@pytest.mark.parametrize("rt", [None, "f32", "bf16"])
+@pytest.mark.parametrize("bits", [8, 6])
+def test_types(xt, rt, bits):
+    _run(5, 1040, xt, rt, "f32", bits)
+    _run(3, 272, xt, rt, "bf16", bits, pad=8)
+
+
+# one block; the last column of one wavefront, its first beyond; every number of steps kept; a row that is read twice
+@pytest.mark.parametrize("cols", [16, 48, 512, 1008, 1024, 1040, 2064, 4096, 4112, 8192, 11008, 16400, 28672, 32768, 32784, 70000 // 16 * 16])
+@pytest.mark.parametrize("rows", [1, 7])
+def test_widths(rows, cols):
+    _run(rows, cols, "f32", "f32", "f32", 8)
+
+
+def test_many_rows_and_strides():
+    _run(1031, 400, "bf16", "f32", "f32", 8, pad=40)
+    _run(513, 4096, "f32", "bf16", "bf16", 6, pad=16)
+
+
+@pytest.mark.parametrize("cols", [64, 4096, 40000])
+def test_residual_updated_in_place(cols):
+    _run(9, cols, "f32", "f32", "f32", 8, inplace=True)
+    _run(9, cols, "bf16", "bf16", "f32", 8, inplace=True)
+
+
+def test_zero_rows_and_zero_eps():
+    def edit(x, r):
+        x[1] = 0
+        x[2, 16:48] = 0
+        if r is not None:
+            r[1] = 0
+            r[2, 16:48] = 0
+    for eps in (0.0, 1e-6, 3.0):
+        _run(4, 96, "f32", None, "f32", 8, eps=eps, edit=edit)
+        _run(4, 2096, "f32", "f32", "f32", 8, eps=eps, edit=edit)
+
+
+def test_large_and_small_numbers():
+    """Squares beyond fp32's range either way: the sum is 64 bits wide."""
+    for gain in (1e25, 1e-25):
+        def edit(x, r):
+            x.mul_(gain)
+        _run(3, 528, "f32", None, "f32", 8, eps=0.0, edit=edit)
+
+
+def test_no_rows():
+    import torch
+    from paper_2402_02446_amd import binding
+    codes, exps, h, v = binding.lqer_rmsnorm_mx(torch.empty(0, 64, device="cuda"), torch.ones(64, device="cuda"))
+    assert codes.shape == (0, 64) and exps.shape == (0, 4) and h is None and v is None
+
+
+def test_feeds_the_linear():
+    """Codes of the norm through lqer_linear_forward_q are the bits of its values through lqer_linear_forward."""
+    import torch
+    from helpers import oracle_layer_big, upload
+    from paper_2402_02446_amd import binding
+    layer, _ = oracle_layer_big(512, 272, 16, seed=3)
+    lin = upload(layer)
+    x = torch.randn(21, 512, device="cuda")
+    codes, exps, _, values = binding.lqer_rmsnorm_mx(x, torch.ones(512, device="cuda"), values=True)
+    assert torch.equal(binding.lqer_linear_forward_q(lin, codes, exps), binding.lqer_linear_forward(lin, values.float()))
+
+
+def test_tensors_that_the_library_cannot_check():
+    import torch
+    from paper_2402_02446_amd import binding
+    x, w = torch.ones(2, 32, device="cuda"), torch.ones(32, device="cuda")
+    for bad in (dict(x=x.cpu()), dict(x=x.double()), dict(weight=w[:16]), dict(residual=x[:1]), dict(x=x.t()), dict(residual=x, h_out=x.bfloat16())):
+        with pytest.raises(ValueError):
+            binding.lqer_rmsnorm_mx(**{**dict(x=x, weight=w), **bad})
+    with pytest.raises(binding.LqerError):
+        binding.lqer_rmsnorm_mx(x[:, 1:17], w[:16].contiguous())         # rows that do not start on 16 bytes
