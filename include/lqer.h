@@ -332,10 +332,12 @@ int lqer_linear_forward_static(const lqer_layer* layer, const float* X_dev, int6
 
 /*
  * ---- Between a block's linears ---------------------------------------------------------------------------------------
- * The calls below are what a served decoder block does between two linear calls: lqer_rmsnorm_mx hands a layer its X_q.
- * The conventions are those above:
+ * The calls below are what a served decoder block does between two linear calls: lqer_rmsnorm_mx hands a layer its X_q,
+ * lqer_adapters_forward adds the low-rank adapters of each request to a layer's Y.  The conventions are those above:
  * asynchronous on the given stream, no allocation, no host synchronisation, capturable in a HIP graph, the same bits
- * on every run; argument errors are reported before anything is launched.
+ * on every run; argument errors are reported before anything is launched.  Lists that live on the device (the adapter of
+ * a token) cannot be checked by the host: an entry out of range is passed over by the
+ * kernels as each call says, and never leads outside the arrays that were handed over.
  */
 
 /* Types of the values that these calls read and write. */
@@ -350,7 +352,7 @@ typedef enum { LQER_F32 = 0, LQER_BF16 = 1 } lqer_type;
  *   cols          multiple of 16; strides in elements, at least cols
  *   elem_bits     8 or 6, codes_dev int8 [rows][cols], exps_dev uint8 [rows][cols/16]: what lqer_linear_forward_q takes
  *   values_dev    NULL, or bf16 [rows][ldv]: the numbers the codes stand for (8 significant bits: exact in bf16), for
- *                 consumers that take no codes
+ *                 consumers that take no codes, as lqer_adapters_forward
  * All pointers 16-byte aligned (exps_dev: any), strides multiples of 16 bytes; LQER_ERR_SHAPE otherwise.  h is the fp32 sum,
  * rounded once more where res_type is bf16 (v is computed from the fp32 sum); the mean and v are computed in 64
  * bits, so that a code is that of the exact v but for the rounding of h.  Inputs must be finite, eps >= 0 (a row of zeros with eps = 0 has
@@ -361,6 +363,30 @@ int lqer_rmsnorm_mx(const void* x_dev, int x_type, int64_t rows, int64_t cols, i
                     const void* weight_dev, int weight_type, float eps,
                     int elem_bits, int8_t* codes_dev, uint8_t* exps_dev, uint16_t* values_dev, int64_t ldv,
                     void* hip_stream);
+
+/*
+ * Low-rank adapters of many requests at once, beside a layer that all of them share: for every token m with adapter
+ * a = ids[m]
+ *        Y_out[m] = Y_in[m] + scales[a] (X[m] A_a^T) B_a^T
+ *   X_dev      bf16 [M][ldx], ldx >= K;  K, ldx multiples of 8
+ *   ids_dev    int32 [M], in any order; a value outside [0, n_adapters) means no adapter: Y_out[m] = Y_in[m]
+ *   A_dev      bf16 [n_adapters][R][K], B_dev bf16 [n_adapters][N][R]: R, a multiple of 8 up to 128, is the rank that
+ *              there is room for
+ *   ranks_dev  int32 [n_adapters], or NULL: every adapter has rank R.  Values are taken into [0, R]; what lies beyond an
+ *              adapter's rank in A and B is neither used nor waited for
+ *   scales_dev fp32 [n_adapters], or NULL: 1
+ *   Y_in_dev   fp32 [M][ldyi], Y_out_dev fp32 [M][ldyo]; the same array (rows without an adapter are then left alone)
+ *              or two that do not overlap; N is any number, ldyi, ldyo >= N and multiples of 4
+ * Pointers 16-byte aligned (ids, ranks, scales: 4).  Products are exact, sums fp32; the projection X A^T enters the second
+ * product in three bf16 terms, its whole 24 bits.  n_adapters at most 8192 (LQER_ERR_UNSUPPORTED).
+ * workspace_dev: at least lqer_adapters_workspace_bytes(M, K, N, R, n_adapters) bytes, 256-byte aligned, scratch.
+ */
+size_t lqer_adapters_workspace_bytes(int64_t M, int64_t K, int64_t N, int R, int n_adapters);
+int lqer_adapters_forward(const uint16_t* X_dev, int64_t M, int64_t K, int64_t ldx, const int32_t* ids_dev,
+                          const uint16_t* A_dev, const uint16_t* B_dev, int n_adapters, int R,
+                          const int32_t* ranks_dev, const float* scales_dev,
+                          const float* Y_in_dev, int64_t ldyi, float* Y_out_dev, int64_t N, int64_t ldyo,
+                          void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Diagnostic, host only (no device call, runs without a GPU): tiles pseudo-random canonical bytes into the device

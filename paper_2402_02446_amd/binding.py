@@ -27,7 +27,7 @@ EXPORTS = ("lqer_status_string", "lqer_quantize_mx", "lqer_build_factors", "lqer
            "lqer_linear_shared_workspace_bytes", "lqer_linear_forward_shared", "lqer_set_wait_limit",
            "lqer_linear_forward_static", "lqer_layer_import_w", "lqer_layer_weight_bits",
            "lqer_int_layer_import", "lqer_int_layer_export", "lqer_quantize_int8_token", "lqer_selftest_layouts",
-           "lqer_rmsnorm_mx")
+           "lqer_rmsnorm_mx", "lqer_adapters_workspace_bytes", "lqer_adapters_forward")
 
 
 class LqerError(RuntimeError):
@@ -117,6 +117,10 @@ def lib() -> C.CDLL:
     f32 = C.c_float
     L.lqer_rmsnorm_mx.restype = i32
     L.lqer_rmsnorm_mx.argtypes = [vp, i32, i64, i64, i64, vp, i64, vp, i64, i32, vp, i32, f32, i32, vp, vp, vp, i64, vp]
+    L.lqer_adapters_workspace_bytes.restype = sz
+    L.lqer_adapters_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
+    L.lqer_adapters_forward.restype = i32
+    L.lqer_adapters_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, i32, i32, vp, vp, vp, i64, vp, i64, i64, vp, sz, vp]
     _lib = L
     return L
 
@@ -448,5 +452,37 @@ def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, ele
                                  None if h is None else residual.data_ptr(), ldr, None if h is None else h.data_ptr(), ldh,
                                  h is not None and h.dtype == bf16, weight.data_ptr(), weight.dtype == bf16, eps, elem_bits,
                                  codes.data_ptr(), exps.data_ptr(), None if v is None else v.data_ptr(), cols, _stream()),
-           "lqer_rmsnorm_mx")
+           "lqer_rmsnorm_mx", "lqer_adapters_workspace_bytes", "lqer_adapters_forward")
     return codes, exps, h, v
+
+
+def lqer_adapters_workspace_bytes(M: int, K: int, N: int, R: int, n_adapters: int) -> int:
+    return int(lib().lqer_adapters_workspace_bytes(M, K, N, R, n_adapters))
+
+
+def _vector(t, name, n, dtype):
+    if t.shape != (n,) or not _typed(t, name, dtype).is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{n}]")
+    return t.data_ptr()
+
+
+def lqer_adapters_forward(X, ids, A, B, Y, out=None, ranks=None, scales=None, workspace=None):
+    """Y + the adapters of every token: X bf16 [M][K], ids int32 [M], A bf16 [n][R][K], B bf16 [n][N][R], Y fp32 [M][N]; ranks int32 [n],
+    scales fp32 [n].  The result is written to `out` (Y itself unless given) and returned."""
+    import torch
+    bf16, f32 = torch.bfloat16, torch.float32
+    out = Y if out is None else out
+    n, R, K = _typed(A, "A", bf16).shape
+    N = Y.shape[1]
+    M = X.shape[0]
+    ldx, ldyi, ldyo = _rows(_typed(X, "X", bf16), "X", K), _rows(_typed(Y, "Y", f32), "Y", N), _rows(_typed(out, "out", f32), "out", N)
+    if _typed(B, "B", bf16).shape != (n, N, R) or not (A.is_contiguous() and B.is_contiguous()) or Y.shape[0] != M or out.shape[0] != M:
+        raise ValueError("A must be [n][R][K] and B [n][N][R], contiguous, and X, Y and out have the same rows")
+    if workspace is None:
+        workspace = torch.empty(max(lib().lqer_adapters_workspace_bytes(M, K, N, R, n), 256), dtype=torch.uint8, device=X.device)
+    _check(lib().lqer_adapters_forward(X.data_ptr(), M, K, ldx, _vector(ids, "ids", M, torch.int32), A.data_ptr(), B.data_ptr(), n, R,
+                                       None if ranks is None else _vector(ranks, "ranks", n, torch.int32),
+                                       None if scales is None else _vector(scales, "scales", n, f32),
+                                       Y.data_ptr(), ldyi, out.data_ptr(), N, ldyo, workspace.data_ptr(), workspace.numel(), _stream()),
+           "lqer_adapters_forward")
+    return out

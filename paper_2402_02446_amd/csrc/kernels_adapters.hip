@@ -1,0 +1,339 @@
+// Low-rank adapters of many requests beside one layer: Y[m] += s_a (X[m] A_a^T) B_a^T with a = ids[m].
+//
+// Two products with a group of tokens of one adapter each: the projection T = X A^T (K long, R wide), split along K so that few groups fill the
+// chip too, its partial sums in the workspace; and Y + T B^T, which adds the partial sums of its group's T up, in order.  What
+// bounds them: with few tokens the bytes of the A and B of the adapters in the batch, each read by one group; with many the
+// bytes of X and of Y in and out.
+//
+// Groups.  Up to 64 tokens every wavefront finds its group by itself: one comparison of all ids with its own (a ballot) gives the
+// tokens of the adapter, and the first of them keeps the workgroup, the others' end.  Beyond, one workgroup sorts the tokens by
+// adapter first and lists tiles of up to 64 of them.  Tokens without an adapter are a group of rank 0: their rows are copied.
+//
+// Matrix instructions: 16 x 16 x 32 bf16, ranks (then output columns) as rows and tokens as columns, so that a lane holds four
+// neighbouring results of one token: 16-byte stores of T and of Y.  The K axis is permuted in chunks of 64, where a lane group owns 32
+// contiguous bytes of a row.  T goes into the second product as three bf16 terms (24 bits): X, A and B are bf16, so every product is
+// exact and the sums are fp32.
+#include "serve.h"
+#include "mx_device.h"
+
+namespace lqer {
+
+namespace {
+
+constexpr int kTile = 64;              // most tokens of a group's tile
+
+struct Group {
+    int adapter;                       // -1: none
+    int count;                         // tokens; 0: nothing to do here
+};
+
+__device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t m) {
+    const int id = a.ids[m];
+    return id >= 0 && id < a.n ? id : -1;
+}
+
+// The group of workgroup column blockIdx.x, its tokens in rows[] (LDS; complete after the next barrier).  Uniform over the workgroup.
+template <bool FEW>
+__device__ __forceinline__ Group find_group(const AdapterArgs& a, int* rows) {
+    if (FEW) {
+        const int lane = threadIdx.x & 63, m = blockIdx.x;
+        const int id = lane < a.M ? adapter_of(a, lane) : -2;
+        const int mine = __builtin_amdgcn_readlane(id, m);
+        const uint64_t same = __ballot(id == mine);
+        if (__builtin_ctzll(same) != m) return {-1, 0};
+        if (threadIdx.x < 64 && id == mine) rows[__popcll(same & ((1ull << lane) - 1))] = lane;
+        return {mine, (int)__popcll(same)};
+    }
+    if ((int)blockIdx.x >= a.list[0]) return {-1, 0};
+    const AdapterTile t = a.tiles[blockIdx.x];
+    if ((int)threadIdx.x < t.count) rows[threadIdx.x] = a.order[t.start + threadIdx.x];
+    return {t.adapter, t.count};
+}
+
+__device__ __forceinline__ int rank_of(const AdapterArgs& a, int adapter) {
+    if (adapter < 0) return 0;
+    return a.ranks ? min(max(a.ranks[adapter], 0), a.R) : a.R;
+}
+
+// T[split][token][rank]: RT tiles of 16 ranks.  FEW: the four wavefronts share a group's chunks of K; otherwise each has 16 of the
+// tile's tokens.
+template <int RT, bool FEW>
+__global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
+    __shared__ int rows[kTile];
+    __shared__ f32x4 part[FEW ? 4 * RT * 64 : 1];
+    const Group gr = find_group<FEW>(a, rows);
+    const int rank = rank_of(a, gr.adapter);
+    if (gr.count == 0 || rank == 0) return;
+    __syncthreads();
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int64_t per = a.k_split, k_lo = blockIdx.y * per, k_hi = min(a.K, k_lo + per);
+    const uint16_t* const A = a.A + (int64_t)gr.adapter * a.R * a.K;
+    float* const T = a.T + (int64_t)blockIdx.y * a.M * a.Rp;
+    for (int t0 = FEW ? 0 : 16 * wave; t0 < gr.count; t0 += FEW ? 16 : kTile) {
+        const int64_t row = rows[min(t0 + i, gr.count - 1)];
+        const uint16_t* const x = a.X + row * a.ldx;
+        f32x4 acc[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int64_t k0 = k_lo + (FEW ? 64 * wave : 0); k0 < k_hi; k0 += FEW ? 256 : 64) {
+            Frag xf[2], af[2][RT];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t k = k0 + 16 * g + 8 * h;
+                const bool in = k < a.K;
+                xf[h].u = u32x4{0, 0, 0, 0};
+                if (in) xf[h].u = *reinterpret_cast<const u32x4*>(x + k);
+#pragma unroll
+                for (int r = 0; r < RT; ++r) {
+                    af[h][r].u = u32x4{0, 0, 0, 0};
+                    if (in && 16 * r + i < rank) af[h][r].u = *reinterpret_cast<const u32x4*>(A + (int64_t)(16 * r + i) * a.K + k);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[r] = mfma16(af[h][r].v, xf[h].v, acc[r]);
+        }
+        if (FEW) {                     // the wavefronts' sums, in order
+#pragma unroll
+            for (int r = 0; r < RT; ++r) part[(wave * RT + r) * 64 + lane] = acc[r];
+            __syncthreads();
+            for (int r = wave; r < RT; r += 4) {
+                f32x4 s = part[r * 64 + lane];
+#pragma unroll
+                for (int w = 1; w < 4; ++w) s += part[(w * RT + r) * 64 + lane];
+                if (t0 + i < gr.count && 16 * r + 4 * g < a.Rp) *reinterpret_cast<f32x4*>(T + row * a.Rp + 16 * r + 4 * g) = s;
+            }
+            __syncthreads();
+        } else if (t0 + i < gr.count) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+                if (16 * r + 4 * g < a.Rp) *reinterpret_cast<f32x4*>(T + row * a.Rp + 16 * r + 4 * g) = acc[r];
+        }
+    }
+}
+
+// Y_out = Y_in + T B^T of one group and 64 NT output columns; KK steps of 32 ranks.
+template <int KK, int NT, bool FEW>
+__global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
+    constexpr int TROWS = FEW ? 16 : kTile;
+    constexpr int LD = 32 * KK + 8;                        // (a row's length in LDS: 16 bytes more than its ranks, off the same banks)
+    __shared__ int rows[kTile];
+    __shared__ __align__(16) uint16_t terms[3][TROWS][LD];
+    const Group gr = find_group<FEW>(a, rows);
+    if (gr.count == 0) return;
+    const int rank = rank_of(a, gr.adapter);
+    if (rank == 0 && a.Y_in == a.Y_out) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    const int64_t n0 = ((int64_t)blockIdx.y * 4 + wave) * 16 * NT;
+    // what comes from far away first
+    Frag b[NT][KK];
+    const uint16_t* const B = a.B + (int64_t)(gr.adapter < 0 ? 0 : gr.adapter) * a.N * a.R;
+#pragma unroll
+    for (int t = 0; t < NT; ++t)
+#pragma unroll
+        for (int k = 0; k < KK; ++k) {
+            const int64_t n = n0 + 16 * t + i;
+            const int r = 32 * k + 8 * g;
+            b[t][k].u = u32x4{0, 0, 0, 0};
+            if (n < a.N && r < rank) b[t][k].u = *reinterpret_cast<const u32x4*>(B + n * a.R + r);
+        }
+    const float scale = rank > 0 && a.scales ? a.scales[gr.adapter] : 1.0f;
+    __syncthreads();
+    if (rank & 7) {                                        // what lies beyond the rank in its last eight may be anything
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int k = 0; k < KK; ++k) {
+                const int left = rank - 32 * k - 8 * g;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (2 * j + 1 >= left) b[t][k].u[j] &= 2 * j >= left ? 0u : 0xFFFFu;
+            }
+    }
+    for (int t0 = 0; t0 < gr.count; t0 += TROWS) {
+        const int here = min(gr.count - t0, TROWS);
+        if (rank > 0) {
+            for (int e = threadIdx.x; e < here * 32 * KK; e += 256) {
+                const int t = e / (32 * KK), r = e % (32 * KK);
+                float v = 0.f;
+                if (r < rank) {
+                    const float* p = a.T + (int64_t)rows[t0 + t] * a.Rp + r;
+                    for (int s = 0; s < a.splits; ++s) v += p[(int64_t)s * a.M * a.Rp];
+                    v *= scale;
+                }
+                const __bf16 t1 = (__bf16)v;
+                const float v2 = v - (float)t1;
+                const __bf16 t2 = (__bf16)v2;
+                const __bf16 t3 = (__bf16)(v2 - (float)t2);
+                terms[0][t][r] = __builtin_bit_cast(uint16_t, t1);
+                terms[1][t][r] = __builtin_bit_cast(uint16_t, t2);
+                terms[2][t][r] = __builtin_bit_cast(uint16_t, t3);
+            }
+            __syncthreads();
+        }
+        for (int tt = 0; tt < here; tt += 16) {
+            const bool on = tt + i < here;
+            const int64_t row = rows[min(t0 + tt + i, gr.count - 1)];
+            f32x4 y[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int64_t n = n0 + 16 * t + 4 * g;
+                const float* p = a.Y_in + row * a.ldyi + n;
+                y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (on && n + 4 <= a.N) y[t] = *reinterpret_cast<const f32x4*>(p);
+                else if (on)
+                    for (int j = 0; j < 3; ++j)
+                        if (n + j < a.N) y[t][j] = p[j];
+            }
+            f32x4 acc[NT];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (rank > 0) {
+#pragma unroll
+                for (int q = 2; q >= 0; --q)
+#pragma unroll
+                    for (int k = 0; k < KK; ++k) {
+                        Frag f;
+                        f.u = *reinterpret_cast<const u32x4*>(&terms[q][tt + i][32 * k + 8 * g]);
+#pragma unroll
+                        for (int t = 0; t < NT; ++t) acc[t] = mfma16(b[t][k].v, f.v, acc[t]);
+                    }
+            }
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const int64_t n = n0 + 16 * t + 4 * g;
+                float* p = a.Y_out + row * a.ldyo + n;
+                if (rank > 0) y[t] += acc[t];
+                if (on && n + 4 <= a.N) *reinterpret_cast<f32x4*>(p) = y[t];
+                else if (on)
+                    for (int j = 0; j < 3; ++j)
+                        if (n + j < a.N) p[j] = y[t][j];
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// Tokens in the order of their adapters (those without one last) and the tiles of up to 64 of them: one workgroup.  The order
+// within an adapter is that of the atomics' arrival; a token's result does not depend on its place.
+__global__ __launch_bounds__(1024) void adapter_sort_kernel(AdapterArgs a) {
+    extern __shared__ int count[];                         // [n + 1], then where each adapter's next token goes
+    __shared__ int sums[2][16];
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6, bins = a.n + 1;
+    for (int b = t; b < bins; b += 1024) count[b] = 0;
+    __syncthreads();
+    for (int64_t m = t; m < a.M; m += 1024) {
+        const int id = adapter_of(a, m);
+        atomicAdd(&count[id < 0 ? a.n : id], 1);
+    }
+    __syncthreads();
+    const int each = (bins + 1023) / 1024, b0 = min(t * each, bins), b1 = min(b0 + each, bins);
+    int tokens = 0, tiles = 0;
+    for (int b = b0; b < b1; ++b) {
+        tokens += count[b];
+        tiles += (count[b] + kTile - 1) / kTile;
+    }
+    int before_tokens = tokens, before_tiles = tiles;      // sums over the threads before this one
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int x = __shfl_up(before_tokens, d), y = __shfl_up(before_tiles, d);
+        if (lane >= d) { before_tokens += x; before_tiles += y; }
+    }
+    if (lane == 63) { sums[0][wave] = before_tokens; sums[1][wave] = before_tiles; }
+    before_tokens -= tokens;
+    before_tiles -= tiles;
+    __syncthreads();
+    int all = 0;
+    for (int w = 0; w < 16; ++w) {
+        if (w < wave) { before_tokens += sums[0][w]; before_tiles += sums[1][w]; }
+        all += sums[1][w];
+    }
+    if (t == 0) a.list[0] = all;
+    for (int b = b0; b < b1; ++b) {
+        const int c = count[b];
+        count[b] = before_tokens;
+        for (int s = 0; s < c; s += kTile)
+            a.tiles[before_tiles++] = AdapterTile{b < a.n ? b : -1, before_tokens + s, min(c - s, kTile), 0};
+        before_tokens += c;
+    }
+    __syncthreads();
+    for (int64_t m = t; m < a.M; m += 1024) {
+        const int id = adapter_of(a, m);
+        a.order[atomicAdd(&count[id < 0 ? a.n : id], 1)] = (int)m;
+    }
+}
+
+template <int RT>
+hipError_t project(const AdapterArgs& a, dim3 grid, bool few, hipStream_t s) {
+    if (few) hipLaunchKernelGGL((adapter_project_kernel<RT, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((adapter_project_kernel<RT, false>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+template <int KK>
+hipError_t expand(const AdapterArgs& a, unsigned groups, bool few, hipStream_t s) {
+    const auto columns = [&](int nt) { return (unsigned)((a.N + 64 * nt - 1) / (64 * nt)); };
+    if (few) {
+        if ((int64_t)groups * columns(4) >= 1024) hipLaunchKernelGGL((adapter_expand_kernel<KK, 4, true>), dim3(groups, columns(4)), dim3(256), 0, s, a);
+        else hipLaunchKernelGGL((adapter_expand_kernel<KK, 1, true>), dim3(groups, columns(1)), dim3(256), 0, s, a);
+    } else {
+        hipLaunchKernelGGL((adapter_expand_kernel<KK, 4, false>), dim3(groups, columns(4)), dim3(256), 0, s, a);
+    }
+    return hipGetLastError();
+}
+
+int64_t most_groups(int64_t M, int n) { return M <= kTile ? M : M / kTile + (M < n + 1 ? M : n + 1); }
+
+}  // namespace
+
+size_t plan_adapters(AdapterArgs& a, void* workspace) {
+    a.Rp = (a.R + 15) / 16 * 16;
+    const bool few = a.M <= kTile;
+    // Parts of K: at least 256 values each, at most 16 parts, and with many tokens no more than give two workgroups to a compute unit
+    int64_t parts = (a.K + 255) / 256;
+    if (parts > 16) parts = 16;
+    if (!few) {
+        const int64_t tiles = (a.M + kTile - 1) / kTile, want = (512 + tiles - 1) / tiles;
+        if (parts > want) parts = want;
+    }
+    a.k_split = ((a.K + parts - 1) / parts + 63) / 64 * 64;
+    a.splits = (int)((a.K + a.k_split - 1) / a.k_split);
+    const auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
+    uint8_t* const base = (uint8_t*)workspace;
+    int64_t at = up((int64_t)a.splits * a.M * a.Rp * 4);
+    a.T = (float*)base;
+    a.list = nullptr;
+    a.tiles = nullptr;
+    a.order = nullptr;
+    if (!few) {
+        a.list = (int*)(base + at);
+        at += 256;
+        a.tiles = (AdapterTile*)(base + at);
+        at += up(most_groups(a.M, a.n) * (int64_t)sizeof(AdapterTile));
+        a.order = (int*)(base + at);
+        at += up(a.M * 4);
+    }
+    return (size_t)at;
+}
+
+hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s) {
+    const bool few = a.M <= kTile;
+    const unsigned groups = (unsigned)most_groups(a.M, a.n);
+    if (!few) {
+        hipLaunchKernelGGL(adapter_sort_kernel, dim3(1), dim3(1024), (size_t)(a.n + 1) * 4, s, a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    const dim3 grid(groups, (unsigned)a.splits);
+    hipError_t e;
+    if (a.R <= 16) e = project<1>(a, grid, few, s);
+    else if (a.R <= 32) e = project<2>(a, grid, few, s);
+    else if (a.R <= 64) e = project<4>(a, grid, few, s);
+    else e = project<8>(a, grid, few, s);
+    if (e != hipSuccess) return e;
+    if (a.R <= 32) return expand<1>(a, groups, few, s);
+    if (a.R <= 64) return expand<2>(a, groups, few, s);
+    return expand<4>(a, groups, few, s);
+}
+
+}  // namespace lqer

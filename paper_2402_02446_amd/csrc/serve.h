@@ -22,4 +22,33 @@ struct NormArgs {
 };
 hipError_t launch_rmsnorm_mx(const NormArgs& a, hipStream_t s);
 
+constexpr int kMaxAdapters = 8192;     // their counts lie in LDS while tokens are sorted
+constexpr int kMaxAdapterRank = 128;
+struct AdapterTile { int adapter, start, count, unused; };       // adapter -1: tokens without one
+struct AdapterArgs {
+    const uint16_t* X;
+    int64_t M, K, ldx;
+    const int32_t* ids;
+    const uint16_t* A;
+    const uint16_t* B;
+    int n, R;
+    const int32_t* ranks;
+    const float* scales;
+    const float* Y_in;
+    int64_t ldyi;
+    float* Y_out;
+    int64_t N, ldyo;
+    // set by plan_adapters
+    int Rp;                // R in whole tiles of 16: T's row length
+    int splits;            // parts of K, of k_split values each
+    int64_t k_split;
+    float* T;              // [splits][M][Rp]
+    int* list;             // more than 64 tokens: number of tiles,
+    AdapterTile* tiles;    // the tiles,
+    int* order;            // and the tokens in their order
+};
+// Lays the call's scratch out and returns its bytes.
+size_t plan_adapters(AdapterArgs& a, void* workspace);
+hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s);
+
 }  // namespace lqer

@@ -11,6 +11,15 @@ bool stride_ok(int64_t ld, int64_t least, int type) { return ld >= least && (ld 
 bool aligned(const void* p, uintptr_t n) { return ((uintptr_t)p & (n - 1)) == 0; }
 constexpr int64_t kMaxGrid = 0x7FFFFFFF;
 
+// The sizes of a call with adapters; false where it does not take them.  (N: the second axis of a grid counts 64 columns.)
+bool adapter_sizes(AdapterArgs& a, int64_t M, int64_t K, int64_t N, int R, int n) {
+    if (M < 0 || M > kMaxGrid / 2 || K <= 0 || (K & 7) != 0 || N < 0 || N > 65535 * 64ll || R <= 0 || R > kMaxAdapterRank || (R & 7) != 0 || n <= 0 ||
+        n > kMaxAdapters)
+        return false;
+    a.M = M; a.K = K; a.N = N; a.R = R; a.n = n;
+    return true;
+}
+
 }  // namespace
 
 extern "C" {
@@ -31,6 +40,31 @@ int lqer_rmsnorm_mx(const void* x_dev, int x_type, int64_t rows, int64_t cols, i
     const NormArgs a{x_dev, residual_dev, h_dev, weight_dev, x_type, res_type, weight_type, rows, cols, ldx, ldr, ldh, ldv, eps, elem_bits,
                      codes_dev, exps_dev, values_dev};
     return launch_rmsnorm_mx(a, (hipStream_t)hip_stream) == hipSuccess ? LQER_OK : LQER_ERR_HIP;
+}
+
+size_t lqer_adapters_workspace_bytes(int64_t M, int64_t K, int64_t N, int R, int n_adapters) {
+    AdapterArgs a{};
+    if (!adapter_sizes(a, M, K, N, R, n_adapters) || M == 0 || N == 0) return 0;
+    return plan_adapters(a, nullptr);
+}
+
+int lqer_adapters_forward(const uint16_t* X_dev, int64_t M, int64_t K, int64_t ldx, const int32_t* ids_dev, const uint16_t* A_dev,
+                          const uint16_t* B_dev, int n_adapters, int R, const int32_t* ranks_dev, const float* scales_dev,
+                          const float* Y_in_dev, int64_t ldyi, float* Y_out_dev, int64_t N, int64_t ldyo, void* workspace_dev,
+                          size_t workspace_bytes, void* hip_stream) {
+    AdapterArgs a{};
+    if (n_adapters > kMaxAdapters || R > kMaxAdapterRank) return LQER_ERR_UNSUPPORTED;
+    if (!adapter_sizes(a, M, K, N, R, n_adapters)) return LQER_ERR_SHAPE;
+    if (M == 0 || N == 0) return LQER_OK;
+    if (!X_dev || !ids_dev || !A_dev || !B_dev || !Y_in_dev || !Y_out_dev) return LQER_ERR_NULL;
+    if (!stride_ok(ldx, K, LQER_BF16) || !aligned(X_dev, 16) || !aligned(A_dev, 16) || !aligned(B_dev, 16)) return LQER_ERR_SHAPE;
+    if (!stride_ok(ldyi, N, LQER_F32) || !stride_ok(ldyo, N, LQER_F32) || !aligned(Y_in_dev, 16) || !aligned(Y_out_dev, 16)) return LQER_ERR_SHAPE;
+    if (!aligned(ids_dev, 4) || !aligned(ranks_dev, 4) || !aligned(scales_dev, 4)) return LQER_ERR_SHAPE;
+    if (Y_in_dev == Y_out_dev && ldyi != ldyo) return LQER_ERR_SHAPE;
+    if (!workspace_dev || !aligned(workspace_dev, 256) || plan_adapters(a, workspace_dev) > workspace_bytes) return LQER_ERR_WORKSPACE;
+    a.X = X_dev; a.ldx = ldx; a.ids = ids_dev; a.A = A_dev; a.B = B_dev; a.ranks = ranks_dev; a.scales = scales_dev;
+    a.Y_in = Y_in_dev; a.ldyi = ldyi; a.Y_out = Y_out_dev; a.ldyo = ldyo;
+    return launch_adapters(a, (hipStream_t)hip_stream) == hipSuccess ? LQER_OK : LQER_ERR_HIP;
 }
 
 }  // extern "C"
