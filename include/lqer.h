@@ -333,10 +333,11 @@ int lqer_linear_forward_static(const lqer_layer* layer, const float* X_dev, int6
 /*
  * ---- Between a block's linears ---------------------------------------------------------------------------------------
  * The calls below are what a served decoder block does between two linear calls: lqer_rmsnorm_mx hands a layer its X_q,
- * lqer_adapters_forward adds the low-rank adapters of each request to a layer's Y.  The conventions are those above:
+ * lqer_adapters_forward adds the low-rank adapters of each request to a layer's Y, lqer_kv4_append and
+ * lqer_kv4_attention keep the block's keys and values as MXINT4 and attend over them.  The conventions are those above:
  * asynchronous on the given stream, no allocation, no host synchronisation, capturable in a HIP graph, the same bits
  * on every run; argument errors are reported before anything is launched.  Lists that live on the device (the adapter of
- * a token) cannot be checked by the host: an entry out of range is passed over by the
+ * a token, slots, page tables, lengths) cannot be checked by the host: an entry out of range is passed over by the
  * kernels as each call says, and never leads outside the arrays that were handed over.
  */
 
@@ -387,6 +388,65 @@ int lqer_adapters_forward(const uint16_t* X_dev, int64_t M, int64_t K, int64_t l
                           const int32_t* ranks_dev, const float* scales_dev,
                           const float* Y_in_dev, int64_t ldyi, float* Y_out_dev, int64_t N, int64_t ldyo,
                           void* workspace_dev, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A paged cache of keys and values in MXINT4 (blocks of 16 along the head dimension, one exponent byte per block: 4.5
+ * bits a value).  The pool is uint8 [pages][kv_heads][lqer_kv4_page_bytes(page_tokens, head_dim)]; a page holds
+ * page_tokens (P, a power of two from 16 to 1024) tokens, and for each head (head_dim D = 64, 128 or 256) a record
+ *        key codes    [P][D/8] words            value codes    [P/4][D/8][4 tokens] words
+ *        key exps     [P][D/16] bytes           value exps     [P/4][D/16][4 tokens] bytes
+ * in the order key codes, value codes, key exps, value exps: P D 9/8 bytes.  A 32-bit word holds the codes e0..e7 of
+ * eight consecutive dimensions of one token as signs and magnitudes: byte i = |e_i| in bits 0-2, the sign of e_(4 + (i + 3) % 4)
+ * in bit 3, |e_(4+i)| in bits 4-6, the sign of e_i in bit 7; a zero has no sign.  The values of four tokens lie side by side because
+ * the product with the weights contracts over tokens: one 16-byte load holds four terms of eight output dimensions.
+ * Pages need no clearing: what no length covers is never used.  lqer_kv4_page_bytes returns 0 for sizes the format does not have.
+ *
+ * lqer_kv4_append quantizes the step's keys and values into the pool:
+ *   k_dev, v_dev  [T][kv_heads][head_dim] with token strides ldk, ldv (elements, >= kv_heads * head_dim, multiples of
+ *                 16 bytes), kv_type; 16-byte aligned
+ *   slots_dev     int32 [T]: page * P + place in the page; each at most once in a call.  A value outside the pool: that token is not stored
+ * Inputs must be finite; a block's exponent byte is at most 247 (maxima of 2^121 and above saturate).
+ */
+size_t lqer_kv4_page_bytes(int page_tokens, int head_dim);
+int lqer_kv4_append(uint8_t* pool_dev, int64_t pages, int page_tokens, int kv_heads, int head_dim,
+                    const void* k_dev, int64_t ldk, const void* v_dev, int64_t ldv, int kv_type, int64_t T,
+                    const int32_t* slots_dev, void* hip_stream);
+
+/*
+ * Attention of a step's queries over such a cache, the step's own tokens appended before:
+ *        o[i][h] = softmax over the visible tokens t (scale q[i][h] . K[t][h'])  V[t][h'],   h' = h / (q_heads / kv_heads)
+ * Request b has the queries cu_q[b] .. cu_q[b+1]-1 and kv_len[b] cached tokens, n = cu_q[b+1] - cu_q[b] of which are
+ * the queries' own: query i stands at position p = kv_len[b] - n + i and sees t <= p (causal; t < kv_len[b] otherwise),
+ * and with window > 0 only t > p - window.  A query that sees nothing has the output 0.
+ *   q_dev       bf16 [Tq][q_heads][head_dim], token stride ldq (multiple of 8), 16-byte aligned
+ *   cu_q_dev    int32 [n_requests + 1], kv_len_dev int32 [n_requests]
+ *   table_dev   int32 [n_requests][table_ld]: page of tokens 0 .. P-1, P .. 2P-1, ..; kv_len is taken as at most
+ *               table_ld * P; a page outside the pool: its tokens are not seen
+ *   max_q, max_kv  what the launch is laid out for: the largest n and kv_len.  Larger ones are computed all the same, smaller
+ *               estimates cost speed
+ *   out_dev     out_type [Tq][q_heads][head_dim], token stride ldo (multiple of 8); rows that no request covers are left alone
+ *   workspace_dev  lqer_kv4_attention_workspace_bytes(...) of the same numbers, 256-byte aligned, scratch
+ * q_heads is a multiple of kv_heads.  Scores, running maxima, sums and outputs are fp32; the weights exp(s - max) enter the product
+ * with V as two bf16 terms (relative 2^-16).
+ */
+typedef struct {
+    int n_requests;
+    int q_heads, kv_heads, head_dim;
+    int page_tokens;
+    int table_ld;
+    int64_t pages;
+    int64_t Tq;            /* rows of q and out */
+    int64_t ldq, ldo;
+    int max_q, max_kv;
+    int causal;            /* 0 or 1 */
+    int window;            /* 0: none */
+    float scale;
+    int out_type;
+} lqer_kv4_shape;
+size_t lqer_kv4_attention_workspace_bytes(const lqer_kv4_shape* shape);
+int lqer_kv4_attention(const lqer_kv4_shape* shape, const uint8_t* pool_dev, const uint16_t* q_dev,
+                       const int32_t* cu_q_dev, const int32_t* kv_len_dev, const int32_t* table_dev,
+                       void* out_dev, void* workspace_dev, size_t workspace_bytes, void* hip_stream);
 
 /*
  * Diagnostic, host only (no device call, runs without a GPU): tiles pseudo-random canonical bytes into the device

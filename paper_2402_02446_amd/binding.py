@@ -27,7 +27,8 @@ EXPORTS = ("lqer_status_string", "lqer_quantize_mx", "lqer_build_factors", "lqer
            "lqer_linear_shared_workspace_bytes", "lqer_linear_forward_shared", "lqer_set_wait_limit",
            "lqer_linear_forward_static", "lqer_layer_import_w", "lqer_layer_weight_bits",
            "lqer_int_layer_import", "lqer_int_layer_export", "lqer_quantize_int8_token", "lqer_selftest_layouts",
-           "lqer_rmsnorm_mx", "lqer_adapters_workspace_bytes", "lqer_adapters_forward")
+           "lqer_rmsnorm_mx", "lqer_adapters_workspace_bytes", "lqer_adapters_forward",
+           "lqer_kv4_page_bytes", "lqer_kv4_append", "lqer_kv4_attention_workspace_bytes", "lqer_kv4_attention")
 
 
 class LqerError(RuntimeError):
@@ -38,6 +39,12 @@ class LqerError(RuntimeError):
 
 class LaunchOpts(C.Structure):
     _fields_ = [("path", C.c_int), ("variant", C.c_int), ("stages", C.c_int)]
+
+
+class Kv4Shape(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("n_requests", "q_heads", "kv_heads", "head_dim", "page_tokens", "table_ld")] + \
+               [(n, C.c_int64) for n in ("pages", "Tq", "ldq", "ldo")] + \
+               [(n, C.c_int) for n in ("max_q", "max_kv", "causal", "window")] + [("scale", C.c_float), ("out_type", C.c_int)]
 
 
 class Config(C.Structure):
@@ -121,6 +128,14 @@ def lib() -> C.CDLL:
     L.lqer_adapters_workspace_bytes.argtypes = [i64, i64, i64, i32, i32]
     L.lqer_adapters_forward.restype = i32
     L.lqer_adapters_forward.argtypes = [vp, i64, i64, i64, vp, vp, vp, i32, i32, vp, vp, vp, i64, vp, i64, i64, vp, sz, vp]
+    L.lqer_kv4_page_bytes.restype = sz
+    L.lqer_kv4_page_bytes.argtypes = [i32, i32]
+    L.lqer_kv4_append.restype = i32
+    L.lqer_kv4_append.argtypes = [vp, i64, i32, i32, i32, vp, i64, vp, i64, i32, i64, vp, vp]
+    L.lqer_kv4_attention_workspace_bytes.restype = sz
+    L.lqer_kv4_attention_workspace_bytes.argtypes = [C.POINTER(Kv4Shape)]
+    L.lqer_kv4_attention.restype = i32
+    L.lqer_kv4_attention.argtypes = [C.POINTER(Kv4Shape), vp, vp, vp, vp, vp, vp, vp, sz, vp]
     _lib = L
     return L
 
@@ -452,7 +467,8 @@ def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, ele
                                  None if h is None else residual.data_ptr(), ldr, None if h is None else h.data_ptr(), ldh,
                                  h is not None and h.dtype == bf16, weight.data_ptr(), weight.dtype == bf16, eps, elem_bits,
                                  codes.data_ptr(), exps.data_ptr(), None if v is None else v.data_ptr(), cols, _stream()),
-           "lqer_rmsnorm_mx", "lqer_adapters_workspace_bytes", "lqer_adapters_forward")
+           "lqer_rmsnorm_mx", "lqer_adapters_workspace_bytes", "lqer_adapters_forward",
+           "lqer_kv4_page_bytes", "lqer_kv4_append", "lqer_kv4_attention_workspace_bytes", "lqer_kv4_attention")
     return codes, exps, h, v
 
 
@@ -485,4 +501,87 @@ def lqer_adapters_forward(X, ids, A, B, Y, out=None, ranks=None, scales=None, wo
                                        None if scales is None else _vector(scales, "scales", n, f32),
                                        Y.data_ptr(), ldyi, out.data_ptr(), N, ldyo, workspace.data_ptr(), workspace.numel(), _stream()),
            "lqer_adapters_forward")
+    return out
+
+
+def lqer_kv4_page_bytes(page_tokens: int, head_dim: int) -> int:
+    return int(lib().lqer_kv4_page_bytes(page_tokens, head_dim))
+
+
+def lqer_kv4_pool(pages: int, kv_heads: int, page_tokens: int, head_dim: int, device="cuda"):
+    """An uncleared pool: uint8 [pages][kv_heads][lqer_kv4_page_bytes]."""
+    import torch
+    size = lqer_kv4_page_bytes(page_tokens, head_dim)
+    if size == 0:
+        raise LqerError(3, "lqer_kv4_pool")
+    return torch.empty((pages, kv_heads, size), dtype=torch.uint8, device=device)
+
+
+def _kv4_pool(pool, head_dim):
+    """(pages, kv_heads, page_tokens) of a pool for heads of that dimension."""
+    import torch
+    if pool.dim() != 3 or not _typed(pool, "pool", torch.uint8).is_contiguous():
+        raise ValueError("pool must be a contiguous [pages][kv_heads][bytes of a page]")
+    pages, heads, size = pool.shape
+    page_tokens = size * 8 // (head_dim * 9)
+    if page_tokens * head_dim * 9 != size * 8:
+        raise ValueError(f"pool holds no whole tokens of {head_dim} dimensions")
+    return pages, heads, page_tokens
+
+
+def _heads(t, name, heads, head_dim):
+    """The token stride of [tokens][heads][head_dim] whose heads lie side by side."""
+    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
+        raise ValueError(f"{name} must be [tokens][{heads}][{head_dim}] with each token's heads side by side")
+    return t.stride(0) if t.shape[0] > 1 else max(heads * head_dim, t.stride(0))
+
+
+def lqer_kv4_append(pool, k, v, slots):
+    """k, v [T][kv_heads][head_dim], both fp32 or both bf16, into the pool's slots (int32 [T]: page * page_tokens + place)."""
+    import torch
+    T, heads, D = k.shape
+    pages, pool_heads, P = _kv4_pool(pool, D)
+    ldk = _heads(_typed(k, "k", torch.float32, torch.bfloat16), "k", pool_heads, D)
+    ldv = _heads(_typed(v, "v", k.dtype), "v", pool_heads, D)
+    if v.shape[0] != T:
+        raise ValueError("k and v must have the same tokens")
+    _check(lib().lqer_kv4_append(pool.data_ptr(), pages, P, heads, D, k.data_ptr(), ldk, v.data_ptr(), ldv, k.dtype == torch.bfloat16, T,
+                                 _vector(slots, "slots", T, torch.int32), _stream()), "lqer_kv4_append")
+
+
+def lqer_kv4_shape(pool, q, cu_q, table, max_q: int, max_kv: int, scale: float, causal: bool = True, window: int = 0, out=None) -> Kv4Shape:
+    """The sizes of a call of lqer_kv4_attention, for lqer_kv4_attention_workspace_bytes."""
+    import torch
+    Tq, q_heads, D = q.shape
+    pages, heads, P = _kv4_pool(pool, D)
+    ldq = _heads(_typed(q, "q", torch.bfloat16), "q", q_heads, D)
+    ldo = q_heads * D if out is None else _heads(out, "out", q_heads, D)
+    if table.dim() != 2 or not _typed(table, "table", torch.int32).is_contiguous():
+        raise ValueError("table must be a contiguous [requests][pages]")
+    return Kv4Shape(table.shape[0], q_heads, heads, D, P, table.shape[1], pages, Tq, ldq, ldo, max_q, max_kv, causal, window, scale,
+                    0 if out is not None and out.dtype == torch.float32 else 1)
+
+
+def lqer_kv4_attention_workspace_bytes(shape: Kv4Shape) -> int:
+    return int(lib().lqer_kv4_attention_workspace_bytes(C.byref(shape)))
+
+
+def lqer_kv4_attention(pool, q, cu_q, kv_len, table, max_q: int, max_kv: int, scale: float, causal: bool = True, window: int = 0, out=None,
+                       workspace=None):
+    """Attention of q bf16 [Tq][q_heads][head_dim] over the pool: request b has rows cu_q[b] .. cu_q[b + 1] - 1 of q, kv_len[b] cached tokens
+    and the pages table[b] (int32 tensors).  Returns out (bf16 unless given, bf16 or fp32)."""
+    import torch
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
+    elif _typed(out, "out", torch.bfloat16, torch.float32).shape != q.shape:
+        raise ValueError("out must have q's shape")
+    sh = lqer_kv4_shape(pool, q, cu_q, table, max_q, max_kv, scale, causal, window, out)
+    n = table.shape[0]
+    need = lib().lqer_kv4_attention_workspace_bytes(C.byref(sh))
+    if workspace is None and need:
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib().lqer_kv4_attention(C.byref(sh), pool.data_ptr(), q.data_ptr(), _vector(cu_q, "cu_q", n + 1, torch.int32),
+                                    _vector(kv_len, "kv_len", n, torch.int32), table.data_ptr(), out.data_ptr(),
+                                    None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream()),
+           "lqer_kv4_attention")
     return out

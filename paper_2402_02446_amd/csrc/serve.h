@@ -51,4 +51,39 @@ struct AdapterArgs {
 size_t plan_adapters(AdapterArgs& a, void* workspace);
 hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s);
 
+// ---- the cache of keys and values in MXINT4 (formats in lqer.h) ------------------------------------------------------------
+struct Kv4AppendArgs {
+    uint8_t* pool;
+    int64_t pages;
+    int P_bits;            // log2 of a page's tokens
+    int heads, D;
+    const void* k;
+    const void* v;
+    int64_t ldk, ldv;
+    int type;
+    int64_t T;
+    const int32_t* slots;
+};
+hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s);
+
+struct Kv4Args {
+    lqer_kv4_shape sh;
+    const uint8_t* pool;
+    const uint16_t* q;
+    const int32_t* cu_q;
+    const int32_t* kv_len;
+    const int32_t* table;
+    void* out;
+    // set by plan_kv4
+    int group;             // query heads of a cached head
+    int P_bits;
+    int row_tiles;         // tiles of query rows (query, head of the group) a request's launch is laid out for
+    int chunk;             // cached tokens of one part of the axis, at least
+    int splits;            // most parts
+    float* part_o;         // [Tq][q_heads][splits][D]: a part's sum of weighted values,
+    float2* part_ml;       // [Tq][q_heads][splits]: its maximum (in units of log 2) and sum of weights
+};
+size_t plan_kv4(Kv4Args& a, void* workspace);
+hipError_t launch_kv4_attention(const Kv4Args& a, hipStream_t s);
+
 }  // namespace lqer

@@ -58,3 +58,51 @@ def test_adapters_workspace(L):
     assert L.lqer_adapters_workspace_bytes(0, 64, 40, 16, 3) == 0 and L.lqer_adapters_workspace_bytes(4, 60, 40, 16, 3) == 0
     # more than 64 tokens are sorted by adapter in the workspace
     assert L.lqer_adapters_workspace_bytes(65, 64, 40, 16, 3) > L.lqer_adapters_workspace_bytes(64, 64, 40, 16, 3)
+
+
+def test_kv4_page_bytes(L):
+    assert L.lqer_kv4_page_bytes(16, 128) == 16 * 128 * 9 // 8 and L.lqer_kv4_page_bytes(1024, 256) == 1024 * 288
+    for P, D in ((8, 128), (24, 128), (2048, 128), (0, 64), (-16, 64), (16, 32), (16, 96), (16, 512)):
+        assert L.lqer_kv4_page_bytes(P, D) == 0
+
+
+def _append(L, **kw):
+    a = dict(pool=P, pages=3, P=16, heads=2, D=64, k=P, ldk=128, v=P, ldv=128, t=1, T=5, slots=P)
+    a.update(kw)
+    return L.lqer_kv4_append(*a.values(), None)
+
+
+@pytest.mark.parametrize("status, bad", [
+    (0, dict(T=0)), (NULL, dict(pool=None)), (NULL, dict(k=None)), (NULL, dict(v=None)), (NULL, dict(slots=None)), (UNSUPPORTED, dict(P=17)),
+    (UNSUPPORTED, dict(D=80)), (UNSUPPORTED, dict(t=2)), (SHAPE, dict(T=-1)), (SHAPE, dict(pages=0)), (SHAPE, dict(pages=1 << 27)),
+    (SHAPE, dict(heads=0)), (SHAPE, dict(heads=1025)), (SHAPE, dict(ldk=120)), (SHAPE, dict(ldv=132)), (SHAPE, dict(k=P + 2)), (SHAPE, dict(v=P + 4)),
+    (SHAPE, dict(pool=P + 8)), (SHAPE, dict(slots=P + 2))])
+def test_kv4_append(L, status, bad):
+    assert _append(L, **bad) == status
+
+
+def _attend(L, ptrs=None, ws=P, ws_bytes=1 << 30, **kw):
+    a = dict(n_requests=2, q_heads=8, kv_heads=2, head_dim=64, page_tokens=16, table_ld=40, pages=100, Tq=2, ldq=512, ldo=512, max_q=1, max_kv=600,
+             causal=1, window=0, scale=0.125, out_type=1)
+    a.update(kw)
+    p = dict(pool=P, q=P, cu=P, kv=P, table=P, out=P)
+    p.update(ptrs or {})
+    return L.lqer_kv4_attention(binding.C.byref(binding.Kv4Shape(*a.values())), *p.values(), ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("status, bad", [
+    (0, dict(Tq=0)), (0, dict(n_requests=0)), (UNSUPPORTED, dict(head_dim=96)), (UNSUPPORTED, dict(page_tokens=2048)), (UNSUPPORTED, dict(out_type=3)),
+    (SHAPE, dict(q_heads=7)), (SHAPE, dict(q_heads=0)), (SHAPE, dict(kv_heads=0)), (SHAPE, dict(n_requests=-1)), (SHAPE, dict(n_requests=65536)),
+    (SHAPE, dict(table_ld=0)), (SHAPE, dict(table_ld=1 << 28)), (SHAPE, dict(Tq=-1)), (SHAPE, dict(Tq=1 << 31)), (SHAPE, dict(pages=0)),
+    (SHAPE, dict(ldq=511)), (SHAPE, dict(ldq=516)), (SHAPE, dict(ldo=504)), (SHAPE, dict(max_q=-1)), (SHAPE, dict(max_kv=-1)), (SHAPE, dict(causal=2)),
+    (SHAPE, dict(window=-1)), (SHAPE, dict(scale=float("nan"))), (NULL, dict(ptrs=dict(pool=None))), (NULL, dict(ptrs=dict(q=None))),
+    (NULL, dict(ptrs=dict(cu=None))), (NULL, dict(ptrs=dict(kv=None))), (NULL, dict(ptrs=dict(table=None))), (NULL, dict(ptrs=dict(out=None))),
+    (SHAPE, dict(ptrs=dict(pool=P + 8))), (SHAPE, dict(ptrs=dict(q=P + 2))), (SHAPE, dict(ptrs=dict(out=P + 4))), (SHAPE, dict(ptrs=dict(table=P + 1))),
+    (WORKSPACE, dict(ws=None)), (WORKSPACE, dict(ws=P + 16)), (WORKSPACE, dict(ws_bytes=16))])
+def test_kv4_attention(L, status, bad):
+    assert _attend(L, **bad) == status
+
+
+def test_kv4_attention_without_a_shape(L):
+    assert L.lqer_kv4_attention(None, P, P, P, P, P, P, P, 0, None) == NULL
+    assert L.lqer_kv4_attention_workspace_bytes(None) == 0
