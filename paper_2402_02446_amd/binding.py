@@ -467,8 +467,7 @@ def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, ele
                                  None if h is None else residual.data_ptr(), ldr, None if h is None else h.data_ptr(), ldh,
                                  h is not None and h.dtype == bf16, weight.data_ptr(), weight.dtype == bf16, eps, elem_bits,
                                  codes.data_ptr(), exps.data_ptr(), None if v is None else v.data_ptr(), cols, _stream()),
-           "lqer_rmsnorm_mx", "lqer_adapters_workspace_bytes", "lqer_adapters_forward",
-           "lqer_kv4_page_bytes", "lqer_kv4_append", "lqer_kv4_attention_workspace_bytes", "lqer_kv4_attention")
+           "lqer_rmsnorm_mx")
     return codes, exps, h, v
 
 
