@@ -134,7 +134,7 @@ __device__ __forceinline__ void values_of_four(u32x4 w, uint32_t exps, int lane_
 }
 
 template <int D>
-__global__ __launch_bounds__(256) void kv4_few_kernel(Kv4Args a) {
+__global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_kernel(Kv4Args a) {
     constexpr int KW = D / 32, NO = D / 16, WAVES = 4;
     __shared__ float join_o[WAVES][16][D + 4];
     __shared__ float join_m[WAVES][16], join_l[WAVES][16];
@@ -154,6 +154,8 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(Kv4Args a) {
         const int64_t out_row = r.first + query;
         const int q_head = head * a.group + row - query * a.group;
         const int begin = kv4_row_begin(a, r, query), end = kv4_row_end(a, r, query);
+        // what every row of the tile sees: from its last row's beginning to its first row's end
+        const int all_begin = kv4_row_begin(a, r, (r.row0 + r.rows - 1) / a.group), all_end = kv4_row_end(a, r, r.row0 / a.group);
         const int lo = (r.lo & ~31) + split * chunk, hi = min(r.hi, lo + chunk);
         Frag q[KW];
         {
@@ -167,9 +169,7 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(Kv4Args a) {
         float m = -__builtin_inff(), l = 0.f;
 
         int page_base = -(1 << 30), page_of_lane = -1;                 // 64 entries of the request's table, one to a lane
-        for (int t0 = lo + 32 * wave; t0 < hi; t0 += 32 * WAVES) {
-            Step<D> step[2];
-            bool there[2];
+        const auto fetch = [&](int t0, Step<D> (&step)[2], bool (&there)[2]) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int t = t0 + 16 * h, index = t >> a.P_bits;
@@ -182,6 +182,14 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(Kv4Args a) {
                 const uint8_t* rec = a.pool + ((int64_t)(there[h] ? page : 0) * a.sh.kv_heads + head) * R.bytes();
                 step[h].load(rec, R, t & ((1 << a.P_bits) - 1), i, g);
             }
+        };
+        Step<D> next[2];
+        bool next_there[2];
+        if (lo + 32 * wave < hi) fetch(lo + 32 * wave, next, next_there);
+        for (int t0 = lo + 32 * wave; t0 < hi; t0 += 32 * WAVES) {
+            Step<D> step[2] = {next[0], next[1]};
+            const bool there[2] = {next_there[0], next_there[1]};
+            if (t0 + 32 * WAVES < hi) fetch(t0 + 32 * WAVES, next, next_there);    // while this step is computed
             f32x4 s[2];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -190,23 +198,21 @@ __global__ __launch_bounds__(256) void kv4_few_kernel(Kv4Args a) {
                 for (int c = 0; c < KW; ++c)
                     s[h] = mfma16(unpack_w8(step[h].k[c / 4][c % 4], kv4_scale((step[h].ke >> (8 * (c / 2))) & 0xFFu)), q[c].v, s[h]);
             }
-            // the values' exponents of tokens that no row sees, and the scores that a row does not see
-            const bool whole = there[0] && there[1];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int t = t0 + 16 * h + 4 * g;
-                s[h] *= to_log2;
-                if (!whole || t0 + 32 > r.hi || t0 < r.lo) {
+            for (int h = 0; h < 2; ++h) s[h] *= to_log2;
+            if (!there[0] || !there[1] || t0 + 32 > all_end || t0 < all_begin) {
+                // a step that reaches some row's limits: the values' exponents of tokens that no row sees, the scores that a row does not see
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (!there[h] || t + j >= r.hi || t + j < r.lo) {
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const int t = t0 + 16 * h + 4 * g + j;
+                        if (!there[h] || t >= r.hi || t < r.lo) {
 #pragma unroll
                             for (int x = 0; x < Step<D>::VW; ++x) step[h].ve[x] &= ~(0xFFu << (8 * j));
                         }
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (!there[h] || t + j >= end || t + j < begin) s[h][j] = -__builtin_inff();
+                        if (!there[h] || t >= end || t < begin) s[h][j] = -__builtin_inff();
+                    }
             }
             float top = m;
 #pragma unroll
