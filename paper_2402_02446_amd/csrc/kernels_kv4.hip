@@ -83,25 +83,30 @@ struct Step {                                     // what a lane reads of 16 cac
     uint32_t ke;
     uint32_t ve[VW];
 
+    // rec, off: uniform; the lane's own offsets are small and the same for every step
     __device__ __forceinline__ void load(const uint8_t* rec, Kv4Record<D> R, int off, int i, int g) {
-        const uint8_t* kp = rec + R.key(off + i) + g * (D / 8);
+        const uint8_t* const kp = rec + R.key(off);
+        const uint8_t* const ep = rec + R.key_exp(off);
+        const uint32_t ko = (uint32_t)(i * (D / 2) + g * (D / 8)), eo = (uint32_t)(i * (D / 16) + g * (D / 64));
         if (D == 64) {
-            const u32x2 w = *reinterpret_cast<const u32x2*>(kp);
+            const u32x2 w = *reinterpret_cast<const u32x2*>(kp + ko);
             k[0] = u32x4{w[0], w[1], 0, 0};
-            ke = *(rec + R.key_exp(off + i) + g);
+            ke = *(ep + eo);
         } else if (D == 128) {
-            k[0] = *reinterpret_cast<const u32x4*>(kp);
-            ke = *reinterpret_cast<const uint16_t*>(rec + R.key_exp(off + i) + 2 * g);
+            k[0] = *reinterpret_cast<const u32x4*>(kp + ko);
+            ke = *reinterpret_cast<const uint16_t*>(ep + eo);
         } else {
-            k[0] = *reinterpret_cast<const u32x4*>(kp);
-            k[KW > 4 ? 1 : 0] = *reinterpret_cast<const u32x4*>(kp + 16);
-            ke = *reinterpret_cast<const uint32_t*>(rec + R.key_exp(off + i) + 4 * g);
+            k[0] = *reinterpret_cast<const u32x4*>(kp + ko);
+            k[KW > 4 ? 1 : 0] = *reinterpret_cast<const u32x4*>(kp + ko + 16);
+            ke = *reinterpret_cast<const uint32_t*>(ep + eo);
         }
+        const uint8_t* const vp = rec + R.value(off / 4);
+        const uint8_t* const xp = rec + R.value_exp(off / 4);
 #pragma unroll
         for (int h = 0; h < VW; ++h) {
-            const int word = D == 64 ? i / 2 : 16 * h + i;
-            v[h] = *reinterpret_cast<const u32x4*>(rec + R.value(off / 4 + g) + word * 16);
-            ve[h] = *reinterpret_cast<const uint32_t*>(rec + R.value_exp(off / 4 + g) + word / 2 * 4);
+            const uint32_t word = (uint32_t)(D == 64 ? i / 2 : 16 * h + i);
+            v[h] = *reinterpret_cast<const u32x4*>(vp + (uint32_t)(g * (2 * D)) + word * 16);
+            ve[h] = *reinterpret_cast<const uint32_t*>(xp + (uint32_t)(g * (D / 4)) + word / 2 * 4);
         }
     }
 };
@@ -138,12 +143,17 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
     constexpr int KW = D / 32, NO = D / 16, WAVES = 4;
     __shared__ float join_o[WAVES][16][D + 4];
     __shared__ float join_m[WAVES][16], join_l[WAVES][16];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
+    // (the wavefront's number as a scalar: its steps, pages and their addresses are then computed once, not by every lane)
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int head = blockIdx.y % a.sh.kv_heads, b = blockIdx.z, split = blockIdx.x;
     Kv4Rows r = kv4_request(a, b);
     const Kv4Record<D> R{a.P_bits};
     const int32_t* const table = a.table + (int64_t)b * a.sh.table_ld;
-    const float to_log2 = a.sh.scale * kLog2e;
+    // scores stay as the product gives them, the factor to units of log 2 goes into the exponential's multiply-add: a negative one turns the
+    // queries' signs instead, so that the largest score is the largest weight
+    // (0 as the smallest normal number: a masked score is minus infinity)
+    const float to_log2 = __builtin_fmaxf(__builtin_fabsf(a.sh.scale) * kLog2e, 0x1p-126f);
+    const uint32_t turn = a.sh.scale < 0.f ? 0x80008000u : 0u;
     for (int row0 = blockIdx.y / a.sh.kv_heads * 16; row0 < r.n * a.group; row0 += a.row_tiles * 16) {
         kv4_tile(a, r, row0, 16);
         int chunk;
@@ -161,7 +171,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
         {
             const uint16_t* p = a.q + out_row * a.sh.ldq + (int64_t)q_head * D + g * (D / 4);
 #pragma unroll
-            for (int c = 0; c < KW; ++c) q[c].u = *reinterpret_cast<const u32x4*>(p + 8 * c);
+            for (int c = 0; c < KW; ++c) q[c].u = *reinterpret_cast<const u32x4*>(p + 8 * c) ^ turn;
         }
         f32x4 o[NO];
 #pragma unroll
@@ -198,15 +208,15 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
                 for (int c = 0; c < KW; ++c)
                     s[h] = mfma16(unpack_w8(step[h].k[c / 4][c % 4], kv4_scale((step[h].ke >> (8 * (c / 2))) & 0xFFu)), q[c].v, s[h]);
             }
-#pragma unroll
-            for (int h = 0; h < 2; ++h) s[h] *= to_log2;
             if (!there[0] || !there[1] || t0 + 32 > all_end || t0 < all_begin) {
                 // a step that reaches some row's limits: the values' exponents of tokens that no row sees, the scores that a row does not see
+                int at = t0;
+                asm volatile("" : "+s"(at));       // (a branch: left alone, the comparisons are done in every step and one of two results taken)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const int t = t0 + 16 * h + 4 * g + j;
+                        const int t = at + 16 * h + 4 * g + j;
                         if (!there[h] || t >= r.hi || t < r.lo) {
 #pragma unroll
                             for (int x = 0; x < Step<D>::VW; ++x) step[h].ve[x] &= ~(0xFFu << (8 * j));
@@ -219,19 +229,20 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
             for (int j = 0; j < 4; ++j) top = __builtin_fmaxf(top, __builtin_fmaxf(s[0][j], s[1][j]));
             top = quad_rows_max(top);
             if (__ballot(top != m)) {
-                const float down = m == -__builtin_inff() ? 0.f : exp2_fast(m - top);
+                const float down = m == -__builtin_inff() ? 0.f : exp2_fast((m - top) * to_log2);
                 l *= down;
 #pragma unroll
                 for (int x = 0; x < NO; ++x) o[x] *= down;
                 m = top;
             }
-            const float base = m == -__builtin_inff() ? 0.f : m;
+            const float base = m == -__builtin_inff() ? 0.f : m * to_log2;
             Frag p, p2;                            // the weights in two bf16 terms
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 4; j += 2) {
-                    const float e0 = exp2_fast(s[h][j] - base), e1 = exp2_fast(s[h][j + 1] - base);
+                    const float e0 = exp2_fast(__builtin_fmaf(s[h][j], to_log2, -base));
+                    const float e1 = exp2_fast(__builtin_fmaf(s[h][j + 1], to_log2, -base));
                     l += e0;
                     l += e1;
                     const uint32_t w = pack_bf16_near(e0, e1);
@@ -255,7 +266,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
         l = quad_rows_sum(l);
         // the wavefronts' parts, joined
         if (g == 0) {
-            join_m[wave][i] = m;
+            join_m[wave][i] = m == -__builtin_inff() ? m : m * to_log2;
             join_l[wave][i] = l;
         }
 #pragma unroll
@@ -298,43 +309,74 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
     }
 }
 
-// The parts of every row, joined in order: a wavefront to a row, 16 rows to a workgroup.
-template <int D>
+// The parts of every row, joined in order: WAVES wavefronts to a row.  A wavefront's lanes hold 4 dimensions of one part or of
+// several neighbouring ones, the factors of up to 64 parts at a time lie in its lanes.
+template <int D, int WAVES>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a) {
-    constexpr int PER = D / 64;                                        // dimensions of a lane
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int head = blockIdx.x % a.sh.kv_heads, b = blockIdx.y;
+    constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;                 // lanes of a part, parts of a wavefront's load
+    __shared__ f32x4 join[4][LANES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = lane % LANES, sub = lane / LANES;
+    const int head = blockIdx.x % a.sh.kv_heads, b = blockIdx.z;
     Kv4Rows r = kv4_request(a, b);
     for (int row0 = blockIdx.x / a.sh.kv_heads * 16; row0 < r.n * a.group; row0 += a.row_tiles * 16) {
         kv4_tile(a, r, row0, 16);
         int chunk;
         const int parts = kv4_parts(a, r, chunk);
-        if (parts <= 1) continue;
-        for (int c = wave; c < r.rows; c += 4) {
-            const int row = r.row0 + c, query = row / a.group;
-            const int64_t orow = r.first + query;
-            const int h = head * a.group + row - query * a.group;
-            const int64_t at = (orow * a.sh.q_heads + h) * a.splits;
-            float top = -__builtin_inff();
-            for (int s = lane; s < parts; s += 64) top = __builtin_fmaxf(top, a.part_ml[at + s].x);
-            top = wave_max(top);
-            float sum[PER] = {}, weights = 0.f;
-            if (top > -__builtin_inff())
-                for (int s = 0; s < parts; ++s) {
-                    const float2 ml = a.part_ml[at + s];
-                    const float f = exp2_fast(ml.x - top);
-                    weights += f * ml.y;
+        const int c = blockIdx.y * (4 / WAVES) + wave / WAVES;         // this wavefront's row of the tile
+        if (parts <= 1) continue;                                      // (uniform over the workgroup: so is every barrier below)
+        const bool on = c < r.rows;
+        const int row = r.row0 + min(c, r.rows - 1), query = row / a.group;
+        const int64_t orow = r.first + query;
+        const int h = head * a.group + row - query * a.group;
+        const int64_t at = (orow * a.sh.q_heads + h) * a.splits;
+        const f32x4* const po = reinterpret_cast<const f32x4*>(a.part_o + at * D) + d;
+        float top = -__builtin_inff();
+        for (int s = lane; s < parts; s += 64) top = __builtin_fmaxf(top, a.part_ml[at + s].x);
+        top = wave_max(top);
+        f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+        float weights = 0.f;
+        for (int s0 = 0; s0 < parts; s0 += 64) {
+            float f = 0.f;
+            if (s0 + lane < parts) {
+                const float2 ml = a.part_ml[at + s0 + lane];
+                f = ml.x > -__builtin_inff() ? exp2_fast(ml.x - top) : 0.f;
+                weights += f * ml.y;
+            }
+            const int here = min(64, parts - s0);
+            for (int s = AT_ONCE * (wave % WAVES); s < here; s += 4 * AT_ONCE * WAVES) {
+                f32x4 v[4];
 #pragma unroll
-                    for (int x = 0; x < PER; ++x) sum[x] += f * a.part_o[(at + s) * D + lane * PER + x];
+                for (int u = 0; u < 4; ++u) {
+                    const int p = min(s + u * AT_ONCE * WAVES + sub, here - 1);
+                    v[u] = po[(int64_t)(s0 + p) * LANES];
                 }
-            const float inv = weights > 0.f ? 1.0f / weights : 0.f;
-            const int64_t o = orow * a.sh.ldo + (int64_t)h * D + lane * PER;
 #pragma unroll
-            for (int x = 0; x < PER; ++x) {
-                if (a.sh.out_type == LQER_F32) ((float*)a.out)[o + x] = sum[x] * inv;
-                else ((__bf16*)a.out)[o + x] = (__bf16)(sum[x] * inv);
+                for (int u = 0; u < 4; ++u) {
+                    const int p = s + u * AT_ONCE * WAVES + sub;
+                    const float w = __shfl(f, p & 63);
+                    if (p < here) sum += w * v[u];
+                }
             }
         }
+#pragma unroll
+        for (int m = 1; m < 64; m <<= 1) weights += __shfl_xor(weights, m);
+#pragma unroll
+        for (int m = LANES; m < 64; m <<= 1)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sum[j] += __shfl_xor(sum[j], m);
+        if (WAVES > 1) {
+            if (sub == 0) join[wave][d] = sum;
+            __syncthreads();
+            sum = join[0][d];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) sum += join[w][d];
+            __syncthreads();
+        }
+        if (!on || sub != 0 || wave % WAVES != 0) continue;
+        sum *= weights > 0.f ? 1.0f / weights : 0.f;
+        const int64_t o = orow * a.sh.ldo + (int64_t)h * D + 4 * d;
+        if (a.sh.out_type == LQER_F32) *reinterpret_cast<f32x4*>((float*)a.out + o) = sum;
+        else *reinterpret_cast<u32x2*>((uint16_t*)a.out + o) = u32x2{pack_bf16_near(sum[0], sum[1]), pack_bf16_near(sum[2], sum[3])};
     }
 }
 
@@ -343,7 +385,9 @@ hipError_t launch_d(const Kv4Args& a, hipStream_t s) {
     const unsigned y = (unsigned)(a.row_tiles * a.sh.kv_heads);
     hipLaunchKernelGGL((kv4_few_kernel<D>), dim3((unsigned)a.splits, y, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-    hipLaunchKernelGGL((kv4_join_kernel<D>), dim3(y, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
+    // a workgroup to a row where it has many parts, or there are few rows; a wavefront otherwise
+    if (a.splits > 8) hipLaunchKernelGGL((kv4_join_kernel<D, 4>), dim3(y, 16, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv4_join_kernel<D, 1>), dim3(y, 4, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
