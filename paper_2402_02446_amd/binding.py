@@ -7,6 +7,7 @@ no fallback: if the shared library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 import numpy as np
@@ -429,18 +430,15 @@ def lqer_set_wait_limit(polls: int):
 
 
 # ---- between a block's linears ------------------------------------------------------------------------------------------
-def _typed(t, name, *dtypes):
-    """The C ABI sees pointers only: what a tensor holds, and that it is on the GPU, is checked here."""
-    if not t.is_cuda or t.dtype not in dtypes:
-        raise ValueError(f"{name} must be a CUDA tensor of {' or '.join(str(d) for d in dtypes)}")
-    return t
+# The C ABI sees pointers only: what a tensor holds, how it is laid out, and that it is on the GPU, is checked here.  These
+# calls take a few microseconds on the GPU for single tokens, so the checks are written to cost little: one condition a tensor.
+def _refuse(name, what):
+    raise ValueError(f"{name} must be {what}")
 
 
-def _rows(t, name, cols):
-    """The row stride of a matrix whose last axis is contiguous and has `cols` values."""
-    if t.dim() != 2 or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
-        raise ValueError(f"{name} must be [rows][{cols}] with contiguous rows")
-    return t.stride(0) if t.shape[0] > 1 else max(cols, t.stride(0))
+def _stride(t, rows, cols):
+    """The row stride of a matrix; a single row has none of its own."""
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
 
 
 def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, elem_bits: int = 8, values: bool = False):
@@ -448,58 +446,72 @@ def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, ele
     h, values): h is h_out (a new tensor of residual's type unless given; residual itself updates in place), None without a residual;
     values is the bf16 tensor of what the codes stand for, or None."""
     import torch
-    f32, bf16 = torch.float32, torch.bfloat16
-    rows, cols = _typed(x, "x", f32, bf16).shape
-    ldx = _rows(x, "x", cols)
-    if _typed(weight, "weight", f32, bf16).shape != (cols,) or not weight.is_contiguous():
-        raise ValueError(f"weight must be [{cols}]")
-    h, ldr, ldh = None, 0, 0
+    L, f32, bf16 = _lib or lib(), torch.float32, torch.bfloat16
+    shape = x.shape
+    if len(shape) != 2 or not x.is_cuda or x.dtype not in (f32, bf16) or (x.stride(1) != 1 and shape[1] > 1):
+        _refuse("x", "fp32 or bf16 [rows][cols] on the GPU, its rows contiguous")
+    rows, cols = shape
+    if weight.shape != (cols,) or not weight.is_cuda or weight.dtype not in (f32, bf16) or not weight.is_contiguous():
+        _refuse("weight", f"a contiguous fp32 or bf16 [{cols}] on the GPU")
+    h = None
+    r_ptr = h_ptr = None
+    ldr = ldh = res_type = 0
     if residual is not None:
-        ldr = _rows(_typed(residual, "residual", f32, bf16), "residual", cols)
-        h = torch.empty((rows, cols), dtype=residual.dtype, device=x.device) if h_out is None else _typed(h_out, "h_out", residual.dtype)
-        ldh = _rows(h, "h_out", cols)
-        if residual.shape[0] != rows or h.shape[0] != rows:
-            raise ValueError("residual and h_out must have x's rows")
-    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
-    exps = torch.empty((rows, cols // 16), dtype=torch.uint8, device=x.device)
-    v = torch.empty((rows, cols), dtype=bf16, device=x.device) if values else None
-    _check(lib().lqer_rmsnorm_mx(x.data_ptr(), x.dtype == bf16, rows, cols, ldx,
-                                 None if h is None else residual.data_ptr(), ldr, None if h is None else h.data_ptr(), ldh,
-                                 h is not None and h.dtype == bf16, weight.data_ptr(), weight.dtype == bf16, eps, elem_bits,
-                                 codes.data_ptr(), exps.data_ptr(), None if v is None else v.data_ptr(), cols, _stream()),
-           "lqer_rmsnorm_mx")
+        if residual.shape != shape or not residual.is_cuda or residual.dtype not in (f32, bf16) or (residual.stride(1) != 1 and cols > 1):
+            _refuse("residual", "fp32 or bf16 of x's shape on the GPU, its rows contiguous")
+        h = residual.new_empty(shape) if h_out is None else h_out
+        if h.shape != shape or not h.is_cuda or h.dtype != residual.dtype or (h.stride(1) != 1 and cols > 1):
+            _refuse("h_out", "of residual's shape and type, on the GPU, its rows contiguous")
+        r_ptr, h_ptr, ldr, ldh, res_type = residual.data_ptr(), h.data_ptr(), _stride(residual, rows, cols), _stride(h, rows, cols), h.dtype == bf16
+    codes = x.new_empty(shape, dtype=torch.int8)
+    exps = x.new_empty((rows, cols // 16), dtype=torch.uint8)
+    v = x.new_empty(shape, dtype=bf16) if values else None
+    st = L.lqer_rmsnorm_mx(x.data_ptr(), x.dtype == bf16, rows, cols, _stride(x, rows, cols), r_ptr, ldr, h_ptr, ldh, res_type,
+                           weight.data_ptr(), weight.dtype == bf16, eps, elem_bits, codes.data_ptr(), exps.data_ptr(),
+                           v.data_ptr() if values else None, cols, _stream())
+    if st:
+        raise LqerError(st, "lqer_rmsnorm_mx")
     return codes, exps, h, v
 
 
+@functools.lru_cache(maxsize=256)
 def lqer_adapters_workspace_bytes(M: int, K: int, N: int, R: int, n_adapters: int) -> int:
     return int(lib().lqer_adapters_workspace_bytes(M, K, N, R, n_adapters))
-
-
-def _vector(t, name, n, dtype):
-    if t.shape != (n,) or not _typed(t, name, dtype).is_contiguous():
-        raise ValueError(f"{name} must be a contiguous [{n}]")
-    return t.data_ptr()
 
 
 def lqer_adapters_forward(X, ids, A, B, Y, out=None, ranks=None, scales=None, workspace=None):
     """Y + the adapters of every token: X bf16 [M][K], ids int32 [M], A bf16 [n][R][K], B bf16 [n][N][R], Y fp32 [M][N]; ranks int32 [n],
     scales fp32 [n].  The result is written to `out` (Y itself unless given) and returned."""
     import torch
-    bf16, f32 = torch.bfloat16, torch.float32
-    out = Y if out is None else out
-    n, R, K = _typed(A, "A", bf16).shape
-    N = Y.shape[1]
-    M = X.shape[0]
-    ldx, ldyi, ldyo = _rows(_typed(X, "X", bf16), "X", K), _rows(_typed(Y, "Y", f32), "Y", N), _rows(_typed(out, "out", f32), "out", N)
-    if _typed(B, "B", bf16).shape != (n, N, R) or not (A.is_contiguous() and B.is_contiguous()) or Y.shape[0] != M or out.shape[0] != M:
-        raise ValueError("A must be [n][R][K] and B [n][N][R], contiguous, and X, Y and out have the same rows")
+    L, bf16, f32, i32 = _lib or lib(), torch.bfloat16, torch.float32, torch.int32
+    n, R, K = A.shape
+    M, N = shape = Y.shape
+    if A.dtype != bf16 or not A.is_cuda or not A.is_contiguous():
+        _refuse("A", "a contiguous bf16 [adapters][rank][K] on the GPU")
+    if B.shape != (n, N, R) or B.dtype != bf16 or not B.is_cuda or not B.is_contiguous():
+        _refuse("B", f"a contiguous bf16 [{n}][{N}][{R}] on the GPU")
+    if X.shape != (M, K) or X.dtype != bf16 or not X.is_cuda or (X.stride(1) != 1 and K > 1):
+        _refuse("X", f"bf16 [{M}][{K}] on the GPU, its rows contiguous")
+    if Y.dtype != f32 or not Y.is_cuda or (Y.stride(1) != 1 and N > 1):
+        _refuse("Y", "fp32 [tokens][N] on the GPU, its rows contiguous")
+    if out is None:
+        out = Y
+    elif out.shape != shape or out.dtype != f32 or not out.is_cuda or (out.stride(1) != 1 and N > 1):
+        _refuse("out", "fp32 of Y's shape on the GPU, its rows contiguous")
+    if ids.shape != (M,) or ids.dtype != i32 or not ids.is_cuda or not ids.is_contiguous():
+        _refuse("ids", f"a contiguous int32 [{M}] on the GPU")
+    if ranks is not None and (ranks.shape != (n,) or ranks.dtype != i32 or not ranks.is_cuda or not ranks.is_contiguous()):
+        _refuse("ranks", f"a contiguous int32 [{n}] on the GPU")
+    if scales is not None and (scales.shape != (n,) or scales.dtype != f32 or not scales.is_cuda or not scales.is_contiguous()):
+        _refuse("scales", f"a contiguous fp32 [{n}] on the GPU")
     if workspace is None:
-        workspace = torch.empty(max(lib().lqer_adapters_workspace_bytes(M, K, N, R, n), 256), dtype=torch.uint8, device=X.device)
-    _check(lib().lqer_adapters_forward(X.data_ptr(), M, K, ldx, _vector(ids, "ids", M, torch.int32), A.data_ptr(), B.data_ptr(), n, R,
-                                       None if ranks is None else _vector(ranks, "ranks", n, torch.int32),
-                                       None if scales is None else _vector(scales, "scales", n, f32),
-                                       Y.data_ptr(), ldyi, out.data_ptr(), N, ldyo, workspace.data_ptr(), workspace.numel(), _stream()),
-           "lqer_adapters_forward")
+        workspace = X.new_empty(max(lqer_adapters_workspace_bytes(M, K, N, R, n), 256), dtype=torch.uint8)
+    st = L.lqer_adapters_forward(X.data_ptr(), M, K, _stride(X, M, K), ids.data_ptr(), A.data_ptr(), B.data_ptr(), n, R,
+                                 None if ranks is None else ranks.data_ptr(), None if scales is None else scales.data_ptr(),
+                                 Y.data_ptr(), _stride(Y, M, N), out.data_ptr(), N, _stride(out, M, N),
+                                 workspace.data_ptr(), workspace.nbytes, _stream())
+    if st:
+        raise LqerError(st, "lqer_adapters_forward")
     return out
 
 
@@ -516,53 +528,68 @@ def lqer_kv4_pool(pages: int, kv_heads: int, page_tokens: int, head_dim: int, de
     return torch.empty((pages, kv_heads, size), dtype=torch.uint8, device=device)
 
 
-def _kv4_pool(pool, head_dim):
+def _kv4_pool(pool, head_dim, u8):
     """(pages, kv_heads, page_tokens) of a pool for heads of that dimension."""
-    import torch
-    if pool.dim() != 3 or not _typed(pool, "pool", torch.uint8).is_contiguous():
-        raise ValueError("pool must be a contiguous [pages][kv_heads][bytes of a page]")
-    pages, heads, size = pool.shape
-    page_tokens = size * 8 // (head_dim * 9)
-    if page_tokens * head_dim * 9 != size * 8:
-        raise ValueError(f"pool holds no whole tokens of {head_dim} dimensions")
-    return pages, heads, page_tokens
+    shape = pool.shape
+    if len(shape) != 3 or pool.dtype != u8 or not pool.is_cuda or not pool.is_contiguous():
+        _refuse("pool", "a contiguous uint8 [pages][kv_heads][bytes of a page] on the GPU")
+    page_tokens = shape[2] * 8 // (head_dim * 9) if head_dim > 0 else 0
+    if page_tokens * head_dim * 9 != shape[2] * 8:
+        _refuse("pool", f"of whole tokens of {head_dim} dimensions")
+    return shape[0], shape[1], page_tokens
 
 
-def _heads(t, name, heads, head_dim):
-    """The token stride of [tokens][heads][head_dim] whose heads lie side by side."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != head_dim or t.stride(2) != 1 or (heads > 1 and t.stride(1) != head_dim):
-        raise ValueError(f"{name} must be [tokens][{heads}][{head_dim}] with each token's heads side by side")
-    return t.stride(0) if t.shape[0] > 1 else max(heads * head_dim, t.stride(0))
+def _side_by_side(t, heads, head_dim):
+    return t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim)
 
 
 def lqer_kv4_append(pool, k, v, slots):
     """k, v [T][kv_heads][head_dim], both fp32 or both bf16, into the pool's slots (int32 [T]: page * page_tokens + place)."""
     import torch
-    T, heads, D = k.shape
-    pages, pool_heads, P = _kv4_pool(pool, D)
-    ldk = _heads(_typed(k, "k", torch.float32, torch.bfloat16), "k", pool_heads, D)
-    ldv = _heads(_typed(v, "v", k.dtype), "v", pool_heads, D)
-    if v.shape[0] != T:
-        raise ValueError("k and v must have the same tokens")
-    _check(lib().lqer_kv4_append(pool.data_ptr(), pages, P, heads, D, k.data_ptr(), ldk, v.data_ptr(), ldv, k.dtype == torch.bfloat16, T,
-                                 _vector(slots, "slots", T, torch.int32), _stream()), "lqer_kv4_append")
+    L, bf16 = _lib or lib(), torch.bfloat16
+    T, heads, D = shape = k.shape
+    dtype = k.dtype
+    pages, pool_heads, P = _kv4_pool(pool, D, torch.uint8)
+    if heads != pool_heads or not k.is_cuda or (dtype != bf16 and dtype != torch.float32) or not _side_by_side(k, heads, D):
+        _refuse("k", f"fp32 or bf16 [tokens][{pool_heads}][head_dim] on the GPU, a token's heads side by side")
+    if v.shape != shape or not v.is_cuda or v.dtype != dtype or not _side_by_side(v, heads, D):
+        _refuse("v", "of k's shape and type, on the GPU, a token's heads side by side")
+    if slots.shape != (T,) or slots.dtype != torch.int32 or not slots.is_cuda or not slots.is_contiguous():
+        _refuse("slots", f"a contiguous int32 [{T}] on the GPU")
+    st = L.lqer_kv4_append(pool.data_ptr(), pages, P, heads, D, k.data_ptr(), _stride(k, T, heads * D), v.data_ptr(),
+                           _stride(v, T, heads * D), dtype == bf16, T, slots.data_ptr(), _stream())
+    if st:
+        raise LqerError(st, "lqer_kv4_append")
 
 
-def lqer_kv4_shape(pool, q, cu_q, table, max_q: int, max_kv: int, scale: float, causal: bool = True, window: int = 0, out=None) -> Kv4Shape:
-    """The sizes of a call of lqer_kv4_attention, for lqer_kv4_attention_workspace_bytes."""
+@functools.lru_cache(maxsize=256)
+def _kv4_sizes(*sizes):
+    """A call's sizes as the library takes them, and the bytes of its workspace."""
+    shape = Kv4Shape(*sizes)
+    return C.byref(shape), int(lib().lqer_kv4_attention_workspace_bytes(C.byref(shape))), shape
+
+
+def _kv4_shape(pool, q, table, max_q, max_kv, scale, causal, window, out):
     import torch
     Tq, q_heads, D = q.shape
-    pages, heads, P = _kv4_pool(pool, D)
-    ldq = _heads(_typed(q, "q", torch.bfloat16), "q", q_heads, D)
-    ldo = q_heads * D if out is None else _heads(out, "out", q_heads, D)
-    if table.dim() != 2 or not _typed(table, "table", torch.int32).is_contiguous():
-        raise ValueError("table must be a contiguous [requests][pages]")
-    return Kv4Shape(table.shape[0], q_heads, heads, D, P, table.shape[1], pages, Tq, ldq, ldo, max_q, max_kv, causal, window, scale,
-                    0 if out is not None and out.dtype == torch.float32 else 1)
+    pages, heads, P = _kv4_pool(pool, D, torch.uint8)
+    if q.dtype != torch.bfloat16 or not q.is_cuda or not _side_by_side(q, q_heads, D):
+        _refuse("q", "bf16 [tokens][q_heads][head_dim] on the GPU, a token's heads side by side")
+    ldo, out_type = q_heads * D, 1
+    if out is not None:
+        out_type = out.dtype == torch.bfloat16
+        if out.shape != q.shape or not out.is_cuda or (not out_type and out.dtype != torch.float32) or not _side_by_side(out, q_heads, D):
+            _refuse("out", "bf16 or fp32 of q's shape on the GPU, a token's heads side by side")
+        ldo = _stride(out, Tq, ldo)
+    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_cuda or not table.is_contiguous():
+        _refuse("table", "a contiguous int32 [requests][pages] on the GPU")
+    n, ld = table.shape
+    return _kv4_sizes(n, q_heads, heads, D, P, ld, pages, Tq, _stride(q, Tq, q_heads * D), ldo, max_q, max_kv, bool(causal), window, scale, out_type)
 
 
-def lqer_kv4_attention_workspace_bytes(shape: Kv4Shape) -> int:
-    return int(lib().lqer_kv4_attention_workspace_bytes(C.byref(shape)))
+def lqer_kv4_attention_workspace_bytes(pool, q, table, max_q: int, max_kv: int, causal: bool = True, window: int = 0) -> int:
+    """Bytes of the workspace of lqer_kv4_attention with tensors and numbers like these."""
+    return _kv4_shape(pool, q, table, max_q, max_kv, 1.0, causal, window, None)[1]
 
 
 def lqer_kv4_attention(pool, q, cu_q, kv_len, table, max_q: int, max_kv: int, scale: float, causal: bool = True, window: int = 0, out=None,
@@ -570,17 +597,19 @@ def lqer_kv4_attention(pool, q, cu_q, kv_len, table, max_q: int, max_kv: int, sc
     """Attention of q bf16 [Tq][q_heads][head_dim] over the pool: request b has rows cu_q[b] .. cu_q[b + 1] - 1 of q, kv_len[b] cached tokens
     and the pages table[b] (int32 tensors).  Returns out (bf16 unless given, bf16 or fp32)."""
     import torch
+    L, i32 = _lib or lib(), torch.int32
+    sizes, need, shape = _kv4_shape(pool, q, table, max_q, max_kv, scale, causal, window, out)
+    n = shape.n_requests
+    if cu_q.shape != (n + 1,) or cu_q.dtype != i32 or not cu_q.is_cuda or not cu_q.is_contiguous():
+        _refuse("cu_q", f"a contiguous int32 [{n + 1}] on the GPU")
+    if kv_len.shape != (n,) or kv_len.dtype != i32 or not kv_len.is_cuda or not kv_len.is_contiguous():
+        _refuse("kv_len", f"a contiguous int32 [{n}] on the GPU")
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.bfloat16, device=q.device)
-    elif _typed(out, "out", torch.bfloat16, torch.float32).shape != q.shape:
-        raise ValueError("out must have q's shape")
-    sh = lqer_kv4_shape(pool, q, cu_q, table, max_q, max_kv, scale, causal, window, out)
-    n = table.shape[0]
-    need = lib().lqer_kv4_attention_workspace_bytes(C.byref(sh))
+        out = q.new_empty(q.shape)
     if workspace is None and need:
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _check(lib().lqer_kv4_attention(C.byref(sh), pool.data_ptr(), q.data_ptr(), _vector(cu_q, "cu_q", n + 1, torch.int32),
-                                    _vector(kv_len, "kv_len", n, torch.int32), table.data_ptr(), out.data_ptr(),
-                                    None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream()),
-           "lqer_kv4_attention")
+        workspace = q.new_empty(need, dtype=torch.uint8)
+    st = L.lqer_kv4_attention(sizes, pool.data_ptr(), q.data_ptr(), cu_q.data_ptr(), kv_len.data_ptr(), table.data_ptr(), out.data_ptr(),
+                              None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream())
+    if st:
+        raise LqerError(st, "lqer_kv4_attention")
     return out

@@ -412,12 +412,12 @@ size_t plan_kv4(Kv4Args& a, void* workspace) {
     int64_t tiles = (rows + 15) / 16;
     const int64_t most_tiles = 65535 / sh.kv_heads;
     a.row_tiles = (int)(tiles < 1 ? 1 : tiles > most_tiles ? most_tiles : tiles);
-    // Parts of the axis: 128 tokens at least (a step of 32 for each wavefront), and so many that about six workgroups come to a compute unit
+    // Parts of the axis: 128 tokens at least (a step of 32 for each wavefront), and about three workgroups to a compute unit, all at work at once
     int64_t seen = sh.max_kv;
     if (sh.window > 0 && (int64_t)sh.window + sh.max_q + 31 < seen) seen = (int64_t)sh.window + sh.max_q + 31;
     if (seen < 1) seen = 1;
     const int64_t lots = (int64_t)sh.n_requests * sh.kv_heads * a.row_tiles;
-    int64_t chunk = (seen * lots / 1536 + 127) / 128 * 128;
+    int64_t chunk = (seen * lots / 768 + 127) / 128 * 128;
     if (chunk < 128) chunk = 128;
     if (chunk > (1 << 30)) chunk = 1 << 30;
     int64_t splits = (seen + chunk - 1) / chunk;

@@ -253,8 +253,7 @@ def test_a_step_captured_in_a_graph(q_lens, lens):
     q = torch.randn(T, heads * G, D, device="cuda").bfloat16()
     k, v = (torch.randn(T, heads, D, device="cuda") for _ in range(2))
     out = torch.empty_like(q)
-    shape = binding.lqer_kv4_shape(pool, q, cu, table_d, max(q_lens), max(lens), D ** -0.5, out=out)
-    ws = torch.empty(max(binding.lqer_kv4_attention_workspace_bytes(shape), 256), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(max(binding.lqer_kv4_attention_workspace_bytes(pool, q, table_d, max(q_lens), max(lens)), 256), dtype=torch.uint8, device="cuda")
 
     def step():
         binding.lqer_kv4_append(pool, k, v, slots)
