@@ -75,24 +75,30 @@ __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
         f32x4 acc[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
-        for (int64_t k0 = k_lo + (FEW ? 64 * wave : 0); k0 < k_hi; k0 += FEW ? 256 : 64) {
-            Frag xf[2], af[2][RT];
+        // AHEAD chunks' loads are issued before the first one's products
+        constexpr int AHEAD = RT <= 2 ? 4 : RT == 4 ? 2 : 1, STEP = FEW ? 256 : 64;
+        for (int64_t k0 = k_lo + (FEW ? 64 * wave : 0); k0 < k_hi; k0 += AHEAD * STEP) {
+            Frag xf[AHEAD][2], af[AHEAD][2][RT];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int64_t k = k0 + 16 * g + 8 * h;
-                const bool in = k < a.K;
-                xf[h].u = u32x4{0, 0, 0, 0};
-                if (in) xf[h].u = *reinterpret_cast<const u32x4*>(x + k);
+            for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    af[h][r].u = u32x4{0, 0, 0, 0};
-                    if (in && 16 * r + i < rank) af[h][r].u = *reinterpret_cast<const u32x4*>(A + (int64_t)(16 * r + i) * a.K + k);
+                for (int h = 0; h < 2; ++h) {
+                    const int64_t k = k0 + u * STEP + 16 * g + 8 * h;
+                    const bool in = k < k_hi;
+                    xf[u][h].u = u32x4{0, 0, 0, 0};
+                    if (in) xf[u][h].u = *reinterpret_cast<const u32x4*>(x + k);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) {
+                        af[u][h][r].u = u32x4{0, 0, 0, 0};
+                        if (in && 16 * r + i < rank) af[u][h][r].u = *reinterpret_cast<const u32x4*>(A + (int64_t)(16 * r + i) * a.K + k);
+                    }
                 }
-            }
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+            for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r] = mfma16(af[h][r].v, xf[h].v, acc[r]);
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) acc[r] = mfma16(af[u][h][r].v, xf[u][h].v, acc[r]);
         }
         if (FEW) {                     // the wavefronts' sums, in order
 #pragma unroll
@@ -113,7 +119,36 @@ __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
     }
 }
 
-// Y_out = Y_in + T B^T of one group and 64 NT output columns; KK steps of 32 ranks.
+// Y_out = Y_in + T B^T of one group and a.columns blocks of 64 NT output columns; KK steps of 32 ranks.
+template <int KK, int NT>
+struct Columns {                                           // a wavefront's B: NT tiles of 16 columns
+    Frag b[NT][KK];
+    __device__ __forceinline__ void load(const AdapterArgs& a, const uint16_t* B, int64_t n0, int rank, int i, int g) {
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int k = 0; k < KK; ++k) {
+                const int64_t n = n0 + 16 * t + i;
+                const int r = 32 * k + 8 * g;
+                b[t][k].u = u32x4{0, 0, 0, 0};
+                if (n < a.N && r < rank) b[t][k].u = *reinterpret_cast<const u32x4*>(B + n * a.R + r);
+            }
+    }
+    // what lies beyond the rank in its last eight may be anything
+    __device__ __forceinline__ void cut(int rank, int g) {
+        if ((rank & 7) == 0) return;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int k = 0; k < KK; ++k) {
+                const int left = rank - 32 * k - 8 * g;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (2 * j + 1 >= left) b[t][k].u[j] &= 2 * j >= left ? 0u : 0xFFFFu;
+            }
+    }
+};
+
 template <int KK, int NT, bool FEW>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
     constexpr int TROWS = FEW ? 16 : kTile;
@@ -125,90 +160,94 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
     const int rank = rank_of(a, gr.adapter);
     if (rank == 0 && a.Y_in == a.Y_out) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int64_t n0 = ((int64_t)blockIdx.y * 4 + wave) * 16 * NT;
-    // what comes from far away first
-    Frag b[NT][KK];
+    const int64_t first = ((int64_t)blockIdx.y * a.columns * 4 + wave) * 16 * NT;
     const uint16_t* const B = a.B + (int64_t)(gr.adapter < 0 ? 0 : gr.adapter) * a.N * a.R;
-#pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int k = 0; k < KK; ++k) {
-            const int64_t n = n0 + 16 * t + i;
-            const int r = 32 * k + 8 * g;
-            b[t][k].u = u32x4{0, 0, 0, 0};
-            if (n < a.N && r < rank) b[t][k].u = *reinterpret_cast<const u32x4*>(B + n * a.R + r);
-        }
+    Columns<KK, NT> next;                                  // what comes from far away first
+    next.load(a, B, first, rank, i, g);
     const float scale = rank > 0 && a.scales ? a.scales[gr.adapter] : 1.0f;
     __syncthreads();
-    if (rank & 7) {                                        // what lies beyond the rank in its last eight may be anything
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int k = 0; k < KK; ++k) {
-                const int left = rank - 32 * k - 8 * g;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (2 * j + 1 >= left) b[t][k].u[j] &= 2 * j >= left ? 0u : 0xFFFFu;
-            }
-    }
     for (int t0 = 0; t0 < gr.count; t0 += TROWS) {
         const int here = min(gr.count - t0, TROWS);
         if (rank > 0) {
-            for (int e = threadIdx.x; e < here * 32 * KK; e += 256) {
-                const int t = e / (32 * KK), r = e % (32 * KK);
-                float v = 0.f;
+            // T: the parts' sums, in order, eight loads at a time; its three bf16 terms
+            for (int e = threadIdx.x; e < here * 8 * KK; e += 256) {
+                const int t = e / (8 * KK), r = e % (8 * KK) * 4;
+                f32x4 v = {0.f, 0.f, 0.f, 0.f};
                 if (r < rank) {
                     const float* p = a.T + (int64_t)rows[t0 + t] * a.Rp + r;
-                    for (int s = 0; s < a.splits; ++s) v += p[(int64_t)s * a.M * a.Rp];
-                    v *= scale;
+                    for (int s0 = 0; s0 < a.splits; s0 += 8) {
+                        f32x4 x[8];
+#pragma unroll
+                        for (int s = 0; s < 8; ++s) x[s] = *reinterpret_cast<const f32x4*>(p + (int64_t)min(s0 + s, a.splits - 1) * a.M * a.Rp);
+#pragma unroll
+                        for (int s = 0; s < 8; ++s)
+                            if (s0 + s < a.splits) v += x[s];
+                    }
                 }
-                const __bf16 t1 = (__bf16)v;
-                const float v2 = v - (float)t1;
-                const __bf16 t2 = (__bf16)v2;
-                const __bf16 t3 = (__bf16)(v2 - (float)t2);
-                terms[0][t][r] = __builtin_bit_cast(uint16_t, t1);
-                terms[1][t][r] = __builtin_bit_cast(uint16_t, t2);
-                terms[2][t][r] = __builtin_bit_cast(uint16_t, t3);
+                uint32_t w[3][2];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float f = r + j < rank ? v[j] * scale : 0.f;
+                    const __bf16 t1 = (__bf16)f;
+                    const float f2 = f - (float)t1;
+                    const __bf16 t2 = (__bf16)f2;
+                    const __bf16 t3 = (__bf16)(f2 - (float)t2);
+                    const uint32_t u[3] = {__builtin_bit_cast(uint16_t, t1), __builtin_bit_cast(uint16_t, t2), __builtin_bit_cast(uint16_t, t3)};
+#pragma unroll
+                    for (int q = 0; q < 3; ++q) w[q][j >> 1] = j & 1 ? w[q][j >> 1] | u[q] << 16 : u[q];
+                }
+#pragma unroll
+                for (int q = 0; q < 3; ++q) *reinterpret_cast<u32x2*>(&terms[q][t][r]) = u32x2{w[q][0], w[q][1]};
             }
             __syncthreads();
         }
-        for (int tt = 0; tt < here; tt += 16) {
-            const bool on = tt + i < here;
-            const int64_t row = rows[min(t0 + tt + i, gr.count - 1)];
-            f32x4 y[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int64_t n = n0 + 16 * t + 4 * g;
-                const float* p = a.Y_in + row * a.ldyi + n;
-                y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (on && n + 4 <= a.N) y[t] = *reinterpret_cast<const f32x4*>(p);
-                else if (on)
-                    for (int j = 0; j < 3; ++j)
-                        if (n + j < a.N) y[t][j] = p[j];
+        for (int c = 0; c < a.columns; ++c) {
+            const int64_t n0 = first + (int64_t)c * 64 * NT;
+            if (n0 >= a.N) break;                          // (of this wavefront alone: no barrier below)
+            Columns<KK, NT> now = next;
+            if (a.columns > 1 || gr.count > TROWS) {       // (the next ones, or the first again for the group's next rows)
+                const int64_t n1 = c + 1 < a.columns ? n0 + 64 * NT : first;
+                next.load(a, B, n1, rank, i, g);
             }
-            f32x4 acc[NT];
+            now.cut(rank, g);
+            for (int tt = 0; tt < here; tt += 16) {
+                const bool on = tt + i < here;
+                const int64_t row = rows[min(t0 + tt + i, gr.count - 1)];
+                f32x4 y[NT];
 #pragma unroll
-            for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-            if (rank > 0) {
+                for (int t = 0; t < NT; ++t) {
+                    const int64_t n = n0 + 16 * t + 4 * g;
+                    const float* p = a.Y_in + row * a.ldyi + n;
+                    y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (on && n + 4 <= a.N) y[t] = *reinterpret_cast<const f32x4*>(p);
+                    else if (on)
+                        for (int j = 0; j < 3; ++j)
+                            if (n + j < a.N) y[t][j] = p[j];
+                }
+                f32x4 acc[NT];
 #pragma unroll
-                for (int q = 2; q >= 0; --q)
+                for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+                if (rank > 0) {
 #pragma unroll
-                    for (int k = 0; k < KK; ++k) {
-                        Frag f;
-                        f.u = *reinterpret_cast<const u32x4*>(&terms[q][tt + i][32 * k + 8 * g]);
+                    for (int q = 2; q >= 0; --q)
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) acc[t] = mfma16(b[t][k].v, f.v, acc[t]);
-                    }
-            }
+                        for (int k = 0; k < KK; ++k) {
+                            Frag f;
+                            f.u = *reinterpret_cast<const u32x4*>(&terms[q][tt + i][32 * k + 8 * g]);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int64_t n = n0 + 16 * t + 4 * g;
-                float* p = a.Y_out + row * a.ldyo + n;
-                if (rank > 0) y[t] += acc[t];
-                if (on && n + 4 <= a.N) *reinterpret_cast<f32x4*>(p) = y[t];
-                else if (on)
-                    for (int j = 0; j < 3; ++j)
-                        if (n + j < a.N) p[j] = y[t][j];
+                            for (int t = 0; t < NT; ++t) acc[t] = mfma16(now.b[t][k].v, f.v, acc[t]);
+                        }
+                }
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const int64_t n = n0 + 16 * t + 4 * g;
+                    float* p = a.Y_out + row * a.ldyo + n;
+                    if (rank > 0) y[t] += acc[t];
+                    if (on && n + 4 <= a.N) *reinterpret_cast<f32x4*>(p) = y[t];
+                    else if (on)
+                        for (int j = 0; j < 3; ++j)
+                            if (n + j < a.N) p[j] = y[t][j];
+                }
             }
         }
         __syncthreads();
@@ -271,16 +310,22 @@ hipError_t project(const AdapterArgs& a, dim3 grid, bool few, hipStream_t s) {
     return hipGetLastError();
 }
 
+template <int KK, int NT, bool FEW>
+hipError_t expand(AdapterArgs a, unsigned groups, hipStream_t s) {
+    // blocks of columns that a workgroup takes one after another, T summed up once for all: as long as about eight workgroups to a compute
+    // unit are left
+    const int64_t blocks = (a.N + 64 * NT - 1) / (64 * NT);
+    int64_t columns = groups * blocks / 2048;
+    a.columns = (int)(columns < 1 ? 1 : columns > blocks ? blocks : columns);
+    const dim3 grid(groups, (unsigned)((blocks + a.columns - 1) / a.columns));
+    hipLaunchKernelGGL((adapter_expand_kernel<KK, NT, FEW>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
 template <int KK>
 hipError_t expand(const AdapterArgs& a, unsigned groups, bool few, hipStream_t s) {
-    const auto columns = [&](int nt) { return (unsigned)((a.N + 64 * nt - 1) / (64 * nt)); };
-    if (few) {
-        if ((int64_t)groups * columns(4) >= 1024) hipLaunchKernelGGL((adapter_expand_kernel<KK, 4, true>), dim3(groups, columns(4)), dim3(256), 0, s, a);
-        else hipLaunchKernelGGL((adapter_expand_kernel<KK, 1, true>), dim3(groups, columns(1)), dim3(256), 0, s, a);
-    } else {
-        hipLaunchKernelGGL((adapter_expand_kernel<KK, 4, false>), dim3(groups, columns(4)), dim3(256), 0, s, a);
-    }
-    return hipGetLastError();
+    if (!few) return expand<KK, 4, false>(a, groups, s);
+    return (int64_t)groups * ((a.N + 255) / 256) >= 1024 ? expand<KK, 4, true>(a, groups, s) : expand<KK, 1, true>(a, groups, s);
 }
 
 int64_t most_groups(int64_t M, int n) { return M <= kTile ? M : M / kTile + (M < n + 1 ? M : n + 1); }

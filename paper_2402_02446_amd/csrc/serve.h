@@ -46,6 +46,8 @@ struct AdapterArgs {
     int* list;             // more than 64 tokens: number of tiles,
     AdapterTile* tiles;    // the tiles,
     int* order;            // and the tokens in their order
+    // set by launch_adapters
+    int columns;           // blocks of columns that a workgroup of the second product takes
 };
 // Lays the call's scratch out and returns its bytes.
 size_t plan_adapters(AdapterArgs& a, void* workspace);
