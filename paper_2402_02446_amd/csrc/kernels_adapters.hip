@@ -24,7 +24,8 @@ constexpr int kTile = 64;              // most tokens of a group's tile
 
 struct Group {
     int adapter;                       // -1: none
-    int count;                         // tokens; 0: nothing to do here
+    int count;                         // tokens
+    int part, parts;                   // this workgroup's share of the group's work; part >= parts: nothing to do
 };
 
 __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t m) {
@@ -32,22 +33,36 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t m) {
     return id >= 0 && id < a.n ? id : -1;
 }
 
-// The group of workgroup column blockIdx.x, its tokens in rows[] (LDS; complete after the next barrier).  Uniform over the workgroup.
+// What this workgroup works on, and its group's tokens in rows[] (LDS).  Uniform over the workgroup; holds barriers.
+// FEW: all workgroups are shared out evenly among the groups that there are; otherwise `parts` to each tile.
 template <bool FEW>
-__device__ __forceinline__ Group find_group(const AdapterArgs& a, int* rows) {
+__device__ __forceinline__ Group find_group(const AdapterArgs& a, int parts, int* rows) {
+    __shared__ Group found;
     if (FEW) {
-        const int lane = threadIdx.x & 63, m = blockIdx.x;
-        const int id = lane < a.M ? adapter_of(a, lane) : -2;
-        const int mine = __builtin_amdgcn_readlane(id, m);
-        const uint64_t same = __ballot(id == mine);
-        if (__builtin_ctzll(same) != m) return {-1, 0};
-        if (threadIdx.x < 64 && id == mine) rows[__popcll(same & ((1ull << lane) - 1))] = lane;
-        return {mine, (int)__popcll(same)};
+        __shared__ uint8_t seen[kMaxAdapters + 1];
+        if (threadIdx.x < 64) {
+            const int lane = threadIdx.x;
+            const bool in = lane < a.M;
+            const int id = in ? adapter_of(a, lane) : -2, at = id < 0 ? a.n : id;
+            // of the tokens of an adapter one finds its own number there: any one of them will do
+            if (in) *(volatile uint8_t*)&seen[at] = (uint8_t)lane;
+            const uint64_t firsts = __ballot(in && *(volatile uint8_t*)&seen[at] == lane);
+            const int groups = (int)__popcll(firsts);
+            const bool mine = ((firsts >> lane) & 1) && (int)__popcll(firsts & ((1ull << lane) - 1)) == (int)(blockIdx.x % groups);
+            const int adapter = __builtin_amdgcn_readlane(id, (int)__builtin_ctzll(__ballot(mine)));
+            const uint64_t same = __ballot(id == adapter);
+            if (id == adapter) rows[__popcll(same & ((1ull << lane) - 1))] = lane;
+            if (lane == 0) found = Group{adapter, (int)__popcll(same), (int)(blockIdx.x / groups), parts > 0 ? parts : (int)(gridDim.x / groups)};
+        }
+    } else {
+        const int tile = (int)(blockIdx.x / parts);
+        if (tile >= a.list[0]) return {-1, 0, 0, 0};
+        const AdapterTile t = a.tiles[tile];
+        if ((int)threadIdx.x < t.count) rows[threadIdx.x] = a.order[t.start + threadIdx.x];
+        if (threadIdx.x == 0) found = Group{t.adapter, t.count, (int)(blockIdx.x % parts), parts};
     }
-    if ((int)blockIdx.x >= a.list[0]) return {-1, 0};
-    const AdapterTile t = a.tiles[blockIdx.x];
-    if ((int)threadIdx.x < t.count) rows[threadIdx.x] = a.order[t.start + threadIdx.x];
-    return {t.adapter, t.count};
+    __syncthreads();
+    return found;
 }
 
 __device__ __forceinline__ int rank_of(const AdapterArgs& a, int adapter) {
@@ -61,14 +76,13 @@ template <int RT, bool FEW>
 __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
     __shared__ int rows[kTile];
     __shared__ f32x4 part[FEW ? 4 * RT * 64 : 1];
-    const Group gr = find_group<FEW>(a, rows);
+    const Group gr = find_group<FEW>(a, a.splits, rows);
     const int rank = rank_of(a, gr.adapter);
-    if (gr.count == 0 || rank == 0) return;
-    __syncthreads();
+    if (gr.part >= gr.parts || rank == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int64_t per = a.k_split, k_lo = blockIdx.y * per, k_hi = min(a.K, k_lo + per);
+    const int64_t per = a.k_split, k_lo = gr.part * per, k_hi = min(a.K, k_lo + per);
     const uint16_t* const A = a.A + (int64_t)gr.adapter * a.R * a.K;
-    float* const T = a.T + (int64_t)blockIdx.y * a.M * a.Rp;
+    float* const T = a.T + (int64_t)gr.part * a.M * a.Rp;
     for (int t0 = FEW ? 0 : 16 * wave; t0 < gr.count; t0 += FEW ? 16 : kTile) {
         const int64_t row = rows[min(t0 + i, gr.count - 1)];
         const uint16_t* const x = a.X + row * a.ldx;
@@ -119,7 +133,7 @@ __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
     }
 }
 
-// Y_out = Y_in + T B^T of one group and a.columns blocks of 64 NT output columns; KK steps of 32 ranks.
+// Y_out = Y_in + T B^T of one group and several blocks of 64 NT output columns; KK steps of 32 ranks.
 template <int KK, int NT>
 struct Columns {                                           // a wavefront's B: NT tiles of 16 columns
     Frag b[NT][KK];
@@ -149,23 +163,41 @@ struct Columns {                                           // a wavefront's B: N
     }
 };
 
+// a lane's four columns of each of NT tiles of a row of Y
+template <int NT>
+__device__ __forceinline__ void read_y(const AdapterArgs& a, f32x4 (&y)[NT], int64_t row, int64_t n0, int g, bool on) {
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int64_t n = n0 + 16 * t + 4 * g;
+        const float* p = a.Y_in + row * a.ldyi + n;
+        y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (on && n + 4 <= a.N) y[t] = *reinterpret_cast<const f32x4*>(p);
+        else if (on)
+            for (int j = 0; j < 3; ++j)
+                if (n + j < a.N) y[t][j] = p[j];
+    }
+}
+
 template <int KK, int NT, bool FEW>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
     constexpr int TROWS = FEW ? 16 : kTile;
     constexpr int LD = 32 * KK + 8;                        // (a row's length in LDS: 16 bytes more than its ranks, off the same banks)
     __shared__ int rows[kTile];
     __shared__ __align__(16) uint16_t terms[3][TROWS][LD];
-    const Group gr = find_group<FEW>(a, rows);
-    if (gr.count == 0) return;
+    const Group gr = find_group<FEW>(a, FEW ? 0 : a.parts, rows);
+    const int blocks = (int)((a.N + 64 * NT - 1) / (64 * NT));
+    const int columns = gr.parts > 0 ? (blocks + gr.parts - 1) / gr.parts : 0;
+    if (gr.part >= gr.parts || (int64_t)gr.part * columns >= blocks) return;
     const int rank = rank_of(a, gr.adapter);
     if (rank == 0 && a.Y_in == a.Y_out) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
-    const int64_t first = ((int64_t)blockIdx.y * a.columns * 4 + wave) * 16 * NT;
+    const int64_t first = ((int64_t)gr.part * columns * 4 + wave) * 16 * NT;
     const uint16_t* const B = a.B + (int64_t)(gr.adapter < 0 ? 0 : gr.adapter) * a.N * a.R;
     Columns<KK, NT> next;                                  // what comes from far away first
     next.load(a, B, first, rank, i, g);
     const float scale = rank > 0 && a.scales ? a.scales[gr.adapter] : 1.0f;
-    __syncthreads();
+    f32x4 y0[NT];
+    read_y<NT>(a, y0, rows[min(i, gr.count - 1)], first, g, i < gr.count);
     for (int t0 = 0; t0 < gr.count; t0 += TROWS) {
         const int here = min(gr.count - t0, TROWS);
         if (rank > 0) {
@@ -201,70 +233,96 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
             }
             __syncthreads();
         }
-        for (int c = 0; c < a.columns; ++c) {
+        // steps of 16 tokens by this wavefront's columns, block by block; a step's Y is loaded during the one before, a block's B during
+        // the whole block before
+        f32x4 y_next[NT];
+        if (t0 > 0) read_y<NT>(a, y_next, rows[min(t0 + i, gr.count - 1)], first, g, i < here);
+        else {
+#pragma unroll
+            for (int t = 0; t < NT; ++t) y_next[t] = y0[t];
+        }
+        Columns<KK, NT> now = next;
+        for (int c = 0, tt = 0; c < columns;) {
             const int64_t n0 = first + (int64_t)c * 64 * NT;
             if (n0 >= a.N) break;                          // (of this wavefront alone: no barrier below)
-            Columns<KK, NT> now = next;
-            if (a.columns > 1 || gr.count > TROWS) {       // (the next ones, or the first again for the group's next rows)
-                const int64_t n1 = c + 1 < a.columns ? n0 + 64 * NT : first;
-                next.load(a, B, n1, rank, i, g);
+            if (tt == 0) {
+                now = next;
+                now.cut(rank, g);
+                const bool more = c + 1 < columns;
+                if (more || t0 + TROWS < gr.count) next.load(a, B, more ? n0 + 64 * NT : first, rank, i, g);
             }
-            now.cut(rank, g);
-            for (int tt = 0; tt < here; tt += 16) {
-                const bool on = tt + i < here;
-                const int64_t row = rows[min(t0 + tt + i, gr.count - 1)];
-                f32x4 y[NT];
+            f32x4 y[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int64_t n = n0 + 16 * t + 4 * g;
-                    const float* p = a.Y_in + row * a.ldyi + n;
-                    y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-                    if (on && n + 4 <= a.N) y[t] = *reinterpret_cast<const f32x4*>(p);
-                    else if (on)
-                        for (int j = 0; j < 3; ++j)
-                            if (n + j < a.N) y[t][j] = p[j];
-                }
-                f32x4 acc[NT];
+            for (int t = 0; t < NT; ++t) y[t] = y_next[t];
+            const bool on = tt + i < here;
+            const int64_t row = rows[min(t0 + tt + i, gr.count - 1)];
+            const int tile = tt;
+            tt += 16;
+            if (tt >= here) { tt = 0; ++c; }
+            if (c < columns) read_y<NT>(a, y_next, rows[min(t0 + tt + i, gr.count - 1)], first + (int64_t)c * 64 * NT, g, tt + i < here);
+            f32x4 acc[NT];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-                if (rank > 0) {
+            for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (rank > 0) {
 #pragma unroll
-                    for (int q = 2; q >= 0; --q)
+                for (int q = 2; q >= 0; --q)
 #pragma unroll
-                        for (int k = 0; k < KK; ++k) {
-                            Frag f;
-                            f.u = *reinterpret_cast<const u32x4*>(&terms[q][tt + i][32 * k + 8 * g]);
+                    for (int k = 0; k < KK; ++k) {
+                        Frag f;
+                        f.u = *reinterpret_cast<const u32x4*>(&terms[q][tile + i][32 * k + 8 * g]);
 #pragma unroll
-                            for (int t = 0; t < NT; ++t) acc[t] = mfma16(now.b[t][k].v, f.v, acc[t]);
-                        }
-                }
+                        for (int t = 0; t < NT; ++t) acc[t] = mfma16(now.b[t][k].v, f.v, acc[t]);
+                    }
+            }
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    const int64_t n = n0 + 16 * t + 4 * g;
-                    float* p = a.Y_out + row * a.ldyo + n;
-                    if (rank > 0) y[t] += acc[t];
-                    if (on && n + 4 <= a.N) *reinterpret_cast<f32x4*>(p) = y[t];
-                    else if (on)
-                        for (int j = 0; j < 3; ++j)
-                            if (n + j < a.N) p[j] = y[t][j];
-                }
+            for (int t = 0; t < NT; ++t) {
+                const int64_t n = n0 + 16 * t + 4 * g;
+                float* p = a.Y_out + row * a.ldyo + n;
+                if (rank > 0) y[t] += acc[t];
+                if (on && n + 4 <= a.N) *reinterpret_cast<f32x4*>(p) = y[t];
+                else if (on)
+                    for (int j = 0; j < 3; ++j)
+                        if (n + j < a.N) p[j] = y[t][j];
             }
         }
         __syncthreads();
     }
 }
 
+// A place in the count of a lane's adapter (id; -2: no token).  Lanes that all have the same one, as in prompts, take theirs with one
+// atomic: 64 on one address wait for each other.
+__device__ __forceinline__ int take_place(int* count, int n, int id) {
+    const int lane = threadIdx.x & 63;
+    const uint64_t in = __ballot(id != -2);
+    if (in == 0) return 0;
+    const int lead = (int)__builtin_ctzll(in), first = __builtin_amdgcn_readlane(id, lead);
+    if (__ballot(id == first) == in) {
+        int base = 0;
+        if (lane == lead) base = atomicAdd(&count[first < 0 ? n : first], (int)__popcll(in));
+        return __builtin_amdgcn_readlane(base, lead) + (int)__popcll(in & ((1ull << lane) - 1));
+    }
+    return id != -2 ? atomicAdd(&count[id < 0 ? n : id], 1) : 0;
+}
+
 // Tokens in the order of their adapters (those without one last) and the tiles of up to 64 of them: one workgroup.  The order
-// within an adapter is that of the atomics' arrival; a token's result does not depend on its place.
+// within an adapter is that of the atomics' arrival; a token's result does not depend on its place.  Up to 8192 tokens each has its place
+// in its adapter's count from the counting itself; beyond, they are read and counted again once the counts' sums are known.
 __global__ __launch_bounds__(1024) void adapter_sort_kernel(AdapterArgs a) {
     extern __shared__ int count[];                         // [n + 1], then where each adapter's next token goes
     __shared__ int sums[2][16];
+    constexpr int EACH = 8;                                // tokens of a thread at a time: their loads go out together
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6, bins = a.n + 1;
     for (int b = t; b < bins; b += 1024) count[b] = 0;
+    int bin[EACH], place[EACH];
     __syncthreads();
-    for (int64_t m = t; m < a.M; m += 1024) {
-        const int id = adapter_of(a, m);
-        atomicAdd(&count[id < 0 ? a.n : id], 1);
+    for (int64_t m0 = 0; m0 < a.M; m0 += 1024 * EACH) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int64_t m = m0 + 1024 * e + t;
+            bin[e] = m < a.M ? adapter_of(a, m) : -2;
+        }
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) place[e] = take_place(count, a.n, bin[e]);
     }
     __syncthreads();
     const int each = (bins + 1023) / 1024, b0 = min(t * each, bins), b1 = min(b0 + each, bins);
@@ -297,47 +355,69 @@ __global__ __launch_bounds__(1024) void adapter_sort_kernel(AdapterArgs a) {
         before_tokens += c;
     }
     __syncthreads();
-    for (int64_t m = t; m < a.M; m += 1024) {
-        const int id = adapter_of(a, m);
-        a.order[atomicAdd(&count[id < 0 ? a.n : id], 1)] = (int)m;
+    if (a.M <= 1024 * EACH) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (bin[e] != -2) a.order[count[bin[e] < 0 ? a.n : bin[e]] + place[e]] = 1024 * e + t;
+        return;
+    }
+    for (int64_t m0 = 0; m0 < a.M; m0 += 1024 * EACH) {
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int64_t m = m0 + 1024 * e + t;
+            bin[e] = m < a.M ? adapter_of(a, m) : -2;
+        }
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            const int at = take_place(count, a.n, bin[e]);
+            if (bin[e] != -2) a.order[at] = (int)(m0 + 1024 * e + t);
+        }
     }
 }
 
+int64_t most_groups(int64_t M, int n) { return M <= kTile ? M : M / kTile + (M < n + 1 ? M : n + 1); }
+
 template <int RT>
-hipError_t project(const AdapterArgs& a, dim3 grid, bool few, hipStream_t s) {
+hipError_t project(const AdapterArgs& a, bool few, hipStream_t s) {
+    const dim3 grid((unsigned)(most_groups(a.M, a.n) * a.splits));
     if (few) hipLaunchKernelGGL((adapter_project_kernel<RT, true>), grid, dim3(256), 0, s, a);
     else hipLaunchKernelGGL((adapter_project_kernel<RT, false>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
+// A workgroup takes several blocks of columns one after another, T summed up once for all, where about eight workgroups
+// to a compute unit are left (few tokens: four, which share the groups that there are out evenly).
 template <int KK, int NT, bool FEW>
-hipError_t expand(AdapterArgs a, unsigned groups, hipStream_t s) {
-    // blocks of columns that a workgroup takes one after another, T summed up once for all: as long as about eight workgroups to a compute
-    // unit are left
-    const int64_t blocks = (a.N + 64 * NT - 1) / (64 * NT);
-    int64_t columns = groups * blocks / 2048;
-    a.columns = (int)(columns < 1 ? 1 : columns > blocks ? blocks : columns);
-    const dim3 grid(groups, (unsigned)((blocks + a.columns - 1) / a.columns));
-    hipLaunchKernelGGL((adapter_expand_kernel<KK, NT, FEW>), grid, dim3(256), 0, s, a);
+hipError_t expand(AdapterArgs a, hipStream_t s) {
+    const int64_t blocks = (a.N + 64 * NT - 1) / (64 * NT), groups = most_groups(a.M, a.n);
+    int64_t grid = groups * blocks;
+    if (FEW) {
+        if (grid > 1024) grid = 1024;              // (more than groups: M <= 64)
+    } else {
+        int64_t columns = grid / 2048;
+        columns = columns < 1 ? 1 : columns > blocks ? blocks : columns;
+        a.parts = (int)((blocks + columns - 1) / columns);
+        grid = groups * a.parts;
+    }
+    hipLaunchKernelGGL((adapter_expand_kernel<KK, NT, FEW>), dim3((unsigned)grid), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
 template <int KK>
-hipError_t expand(const AdapterArgs& a, unsigned groups, bool few, hipStream_t s) {
-    if (!few) return expand<KK, 4, false>(a, groups, s);
-    return (int64_t)groups * ((a.N + 255) / 256) >= 1024 ? expand<KK, 4, true>(a, groups, s) : expand<KK, 1, true>(a, groups, s);
+hipError_t expand(const AdapterArgs& a, bool few, hipStream_t s) {
+    if (!few) return expand<KK, KK == 4 ? 2 : 4, false>(a, s);     // (ranks above 64: fewer columns, or their B leaves one wavefront a SIMD)
+    return a.M * ((a.N + 127) / 128) >= 1024 ? expand<KK, 2, true>(a, s) : expand<KK, 1, true>(a, s);
 }
-
-int64_t most_groups(int64_t M, int n) { return M <= kTile ? M : M / kTile + (M < n + 1 ? M : n + 1); }
 
 }  // namespace
 
 size_t plan_adapters(AdapterArgs& a, void* workspace) {
     a.Rp = (a.R + 15) / 16 * 16;
     const bool few = a.M <= kTile;
-    // Parts of K: at least 256 values each, at most 16 parts, and with many tokens no more than give two workgroups to a compute unit
-    int64_t parts = (a.K + 255) / 256;
-    if (parts > 16) parts = 16;
+    // Parts of K: at least 512 values each, at most 8 parts (that many loads sum T up at once), and with many tokens no more than give two
+    // workgroups to a compute unit
+    int64_t parts = (a.K + 511) / 512;
+    if (parts > 8) parts = 8;
     if (!few) {
         const int64_t tiles = (a.M + kTile - 1) / kTile, want = (512 + tiles - 1) / tiles;
         if (parts > want) parts = want;
@@ -364,21 +444,19 @@ size_t plan_adapters(AdapterArgs& a, void* workspace) {
 
 hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s) {
     const bool few = a.M <= kTile;
-    const unsigned groups = (unsigned)most_groups(a.M, a.n);
     if (!few) {
         hipLaunchKernelGGL(adapter_sort_kernel, dim3(1), dim3(1024), (size_t)(a.n + 1) * 4, s, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
-    const dim3 grid(groups, (unsigned)a.splits);
     hipError_t e;
-    if (a.R <= 16) e = project<1>(a, grid, few, s);
-    else if (a.R <= 32) e = project<2>(a, grid, few, s);
-    else if (a.R <= 64) e = project<4>(a, grid, few, s);
-    else e = project<8>(a, grid, few, s);
+    if (a.R <= 16) e = project<1>(a, few, s);
+    else if (a.R <= 32) e = project<2>(a, few, s);
+    else if (a.R <= 64) e = project<4>(a, few, s);
+    else e = project<8>(a, few, s);
     if (e != hipSuccess) return e;
-    if (a.R <= 32) return expand<1>(a, groups, few, s);
-    if (a.R <= 64) return expand<2>(a, groups, few, s);
-    return expand<4>(a, groups, few, s);
+    if (a.R <= 32) return expand<1>(a, few, s);
+    if (a.R <= 64) return expand<2>(a, few, s);
+    return expand<4>(a, few, s);
 }
 
 }  // namespace lqer

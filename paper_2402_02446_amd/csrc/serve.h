@@ -47,7 +47,7 @@ struct AdapterArgs {
     AdapterTile* tiles;    // the tiles,
     int* order;            // and the tokens in their order
     // set by launch_adapters
-    int columns;           // blocks of columns that a workgroup of the second product takes
+    int parts;             // workgroups of the second product to a tile
 };
 // Lays the call's scratch out and returns its bytes.
 size_t plan_adapters(AdapterArgs& a, void* workspace);

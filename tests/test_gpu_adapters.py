@@ -111,6 +111,13 @@ def test_beyond_an_adapters_rank_anything_may_stand(M):
     _check(d, out)
 
 
+def test_more_tokens_than_are_sorted_at_once():
+    d = _data(8192 + 500, 16, 12, 8, 5)
+    _check(d, _run(d))
+    d = _data(8192, 16, 12, 8, 700)
+    _check(d, _run(d))
+
+
 def test_defaults():
     d = _data(30, 96, 64, 16, 3)
     _check(d, _run(d, ranks=None, scales=None), ranks=False, scales=False)
