@@ -9,8 +9,9 @@
 // tokens of the adapter, and the first of them keeps the workgroup, the others' end.  Beyond, one workgroup sorts the tokens by
 // adapter first and lists tiles of up to 64 of them.  Tokens without an adapter are a group of rank 0: their rows are copied.
 //
-// Matrix instructions: 16 x 16 x 32 bf16, ranks (then output columns) as rows and tokens as columns, so that a lane holds four
-// neighbouring results of one token: 16-byte stores of T and of Y.  The K axis is permuted in chunks of 64, where a lane group owns 32
+// Matrix instructions: 16 x 16 x 32 bf16.  Projection: ranks as rows and tokens as columns, so that a lane holds four neighbouring ranks
+// of one token.  Second product: tokens as rows and as columns every NT-th output column, so that a lane holds NT neighbouring columns
+// and 16 lanes a run of them: Y is read and written in whole cache lines.  The K axis is permuted in chunks of 64, where a lane group owns 32
 // contiguous bytes of a row.  T goes into the second product as three bf16 terms (24 bits): X, A and B are bf16, so every product is
 // exact and the sums are fp32.
 #include "serve.h"
@@ -135,14 +136,14 @@ __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
 
 // Y_out = Y_in + T B^T of one group and several blocks of 64 NT output columns; KK steps of 32 ranks.
 template <int KK, int NT>
-struct Columns {                                           // a wavefront's B: NT tiles of 16 columns
+struct Columns {                                           // a wavefront's B: NT tiles of 16 columns, every NT-th one from the t-th on
     Frag b[NT][KK];
     __device__ __forceinline__ void load(const AdapterArgs& a, const uint16_t* B, int64_t n0, int rank, int i, int g) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
             for (int k = 0; k < KK; ++k) {
-                const int64_t n = n0 + 16 * t + i;
+                const int64_t n = n0 + NT * i + t;
                 const int r = 32 * k + 8 * g;
                 b[t][k].u = u32x4{0, 0, 0, 0};
                 if (n < a.N && r < rank) b[t][k].u = *reinterpret_cast<const u32x4*>(B + n * a.R + r);
@@ -163,20 +164,41 @@ struct Columns {                                           // a wavefront's B: N
     }
 };
 
-// a lane's four columns of each of NT tiles of a row of Y
+// A lane's NT neighbouring columns of the four rows 4 g .. 4 g + 3 of a step's 16 tokens: 16 lanes are NT cache lines of a row.
 template <int NT>
-__device__ __forceinline__ void read_y(const AdapterArgs& a, f32x4 (&y)[NT], int64_t row, int64_t n0, int g, bool on) {
+struct FourRows {
+    float y[4][NT];
+    typedef float vec __attribute__((ext_vector_type(NT)));
+
+    // rows: the step's tokens, `count` of them
+    template <bool STORE, typename P>
+    __device__ __forceinline__ void move(P* base, int64_t ld, const int* rows, int count, int64_t n, int64_t N, int g) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t n = n0 + 16 * t + 4 * g;
-        const float* p = a.Y_in + row * a.ldyi + n;
-        y[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (on && n + 4 <= a.N) y[t] = *reinterpret_cast<const f32x4*>(p);
-        else if (on)
-            for (int j = 0; j < 3; ++j)
-                if (n + j < a.N) y[t][j] = p[j];
+        for (int j = 0; j < 4; ++j) {
+            if (4 * g + j >= count) continue;
+            P* p = base + rows[4 * g + j] * ld + n;
+            if (n + NT <= N) {
+                if constexpr (STORE) {
+                    vec v;
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) v[t] = y[j][t];
+                    *reinterpret_cast<vec*>(p) = v;
+                } else {
+                    const vec v = *reinterpret_cast<const vec*>(p);
+#pragma unroll
+                    for (int t = 0; t < NT; ++t) y[j][t] = v[t];
+                }
+            } else {
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    if (n + t < N) {
+                        if constexpr (STORE) p[t] = y[j][t];
+                        else y[j][t] = p[t];
+                    }
+            }
+        }
     }
-}
+};
 
 template <int KK, int NT, bool FEW>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
@@ -196,8 +218,8 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
     Columns<KK, NT> next;                                  // what comes from far away first
     next.load(a, B, first, rank, i, g);
     const float scale = rank > 0 && a.scales ? a.scales[gr.adapter] : 1.0f;
-    f32x4 y0[NT];
-    read_y<NT>(a, y0, rows[min(i, gr.count - 1)], first, g, i < gr.count);
+    FourRows<NT> y_next;
+    y_next.template move<false>(a.Y_in, a.ldyi, rows, min(gr.count, 16), first + NT * i, a.N, g);
     for (int t0 = 0; t0 < gr.count; t0 += TROWS) {
         const int here = min(gr.count - t0, TROWS);
         if (rank > 0) {
@@ -235,12 +257,7 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
         }
         // steps of 16 tokens by this wavefront's columns, block by block; a step's Y is loaded during the one before, a block's B during
         // the whole block before
-        f32x4 y_next[NT];
-        if (t0 > 0) read_y<NT>(a, y_next, rows[min(t0 + i, gr.count - 1)], first, g, i < here);
-        else {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) y_next[t] = y0[t];
-        }
+        if (t0 > 0) y_next.template move<false>(a.Y_in, a.ldyi, rows + t0, min(here, 16), first + NT * i, a.N, g);
         Columns<KK, NT> now = next;
         for (int c = 0, tt = 0; c < columns;) {
             const int64_t n0 = first + (int64_t)c * 64 * NT;
@@ -251,19 +268,16 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
                 const bool more = c + 1 < columns;
                 if (more || t0 + TROWS < gr.count) next.load(a, B, more ? n0 + 64 * NT : first, rank, i, g);
             }
-            f32x4 y[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) y[t] = y_next[t];
-            const bool on = tt + i < here;
-            const int64_t row = rows[min(t0 + tt + i, gr.count - 1)];
+            FourRows<NT> y = y_next;
             const int tile = tt;
             tt += 16;
             if (tt >= here) { tt = 0; ++c; }
-            if (c < columns) read_y<NT>(a, y_next, rows[min(t0 + tt + i, gr.count - 1)], first + (int64_t)c * 64 * NT, g, tt + i < here);
-            f32x4 acc[NT];
-#pragma unroll
-            for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            if (c < columns)
+                y_next.template move<false>(a.Y_in, a.ldyi, rows + t0 + tt, min(here - tt, 16), first + (int64_t)c * 64 * NT + NT * i, a.N, g);
             if (rank > 0) {
+                f32x4 acc[NT];
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int q = 2; q >= 0; --q)
 #pragma unroll
@@ -271,19 +285,14 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
                         Frag f;
                         f.u = *reinterpret_cast<const u32x4*>(&terms[q][tile + i][32 * k + 8 * g]);
 #pragma unroll
-                        for (int t = 0; t < NT; ++t) acc[t] = mfma16(now.b[t][k].v, f.v, acc[t]);
+                        for (int t = 0; t < NT; ++t) acc[t] = mfma16(f.v, now.b[t][k].v, acc[t]);
                     }
-            }
 #pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int64_t n = n0 + 16 * t + 4 * g;
-                float* p = a.Y_out + row * a.ldyo + n;
-                if (rank > 0) y[t] += acc[t];
-                if (on && n + 4 <= a.N) *reinterpret_cast<f32x4*>(p) = y[t];
-                else if (on)
-                    for (int j = 0; j < 3; ++j)
-                        if (n + j < a.N) p[j] = y[t][j];
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) y.y[j][t] += acc[t][j];
             }
+            y.template move<true>(a.Y_out, a.ldyo, rows + t0 + tile, min(here - tile, 16), n0 + NT * i, a.N, g);
         }
         __syncthreads();
     }
