@@ -14,6 +14,8 @@
 // A part of the axis goes to a workgroup, whose four wavefronts take every fourth step and join in LDS; parts are joined
 // by a second kernel, in order.  Masks are applied where a step reaches a row's limits only.  Tokens beyond the lengths may hold anything:
 // their scores are replaced, and the exponents of their values cleared, so that a weight of 0 meets a finite number.
+#include <algorithm>
+
 #include "kv4_device.h"
 
 namespace lqer {
@@ -147,6 +149,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
     const int head = blockIdx.y % a.sh.kv_heads, b = blockIdx.z, split = blockIdx.x;
     Kv4Rows r = kv4_request(a, b);
+    if (!kv4_mine<false>(a, r)) return;
     const Kv4Record<D> R{a.P_bits};
     const int32_t* const table = a.table + (int64_t)b * a.sh.table_ld;
     // scores stay as the product gives them, the factor to units of log 2 goes into the exponential's multiply-add: a negative one turns the
@@ -154,10 +157,10 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
     // (0 as the smallest normal number: a masked score is minus infinity)
     const float to_log2 = __builtin_fmaxf(__builtin_fabsf(a.sh.scale) * kLog2e, 0x1p-126f);
     const uint32_t turn = a.sh.scale < 0.f ? 0x80008000u : 0u;
-    for (int row0 = blockIdx.y / a.sh.kv_heads * 16; row0 < r.n * a.group; row0 += a.row_tiles * 16) {
+    for (int row0 = blockIdx.y / a.sh.kv_heads * 16; row0 < r.n * a.group; row0 += a.few.row_tiles * 16) {
         kv4_tile(a, r, row0, 16);
         int chunk;
-        const int parts = kv4_parts(a, r, chunk);
+        const int parts = kv4_parts<false>(a, r, chunk);
         if (split >= parts && split > 0) continue;
         // this lane's column
         const int row = r.row0 + min(i, r.rows - 1), query = row / a.group;
@@ -295,9 +298,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
             const int64_t orow = r.first + qu;
             const int h = head * a.group + rr - qu * a.group;
             if (parts > 1) {
-                const int64_t at = (orow * a.sh.q_heads + h) * a.splits + split;
-                *reinterpret_cast<f32x4*>(a.part_o + at * D + d) = sum;
-                if (d == 0) a.part_ml[at] = float2{top, weights};
+                const int64_t at = kv4_part<false>(a, b, head, rr, orow, h) + split;
+                *reinterpret_cast<f32x4*>(a.few.part_o + at * D + d) = sum;
+                if (d == 0) a.few.part_ml[at] = float2{top, weights};
             } else {
                 sum *= weights > 0.f ? 1.0f / weights : 0.f;
                 const int64_t at = orow * a.sh.ldo + (int64_t)h * D + d;
@@ -311,34 +314,37 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
 
 // The parts of every row, joined in order: WAVES wavefronts to a row.  A wavefront's lanes hold 4 dimensions of one part or of
 // several neighbouring ones, the factors of up to 64 parts at a time lie in its lanes.
-template <int D, int WAVES>
+template <int D, int WAVES, bool MANY>
 __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a) {
+    constexpr int ROWS = MANY ? kManyRows : 16;
+    const Kv4Plan& plan = MANY ? a.many : a.few;
     constexpr int LANES = D / 4, AT_ONCE = 64 / LANES;                 // lanes of a part, parts of a wavefront's load
     __shared__ f32x4 join[4][LANES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), d = lane % LANES, sub = lane / LANES;
     const int head = blockIdx.x % a.sh.kv_heads, b = blockIdx.z;
     Kv4Rows r = kv4_request(a, b);
-    for (int row0 = blockIdx.x / a.sh.kv_heads * 16; row0 < r.n * a.group; row0 += a.row_tiles * 16) {
-        kv4_tile(a, r, row0, 16);
+    if (!kv4_mine<MANY>(a, r)) return;
+    for (int row0 = blockIdx.x / a.sh.kv_heads * ROWS; row0 < r.n * a.group; row0 += plan.row_tiles * ROWS) {
+        kv4_tile(a, r, row0, ROWS);
         int chunk;
-        const int parts = kv4_parts(a, r, chunk);
+        const int parts = kv4_parts<MANY>(a, r, chunk);
         const int c = blockIdx.y * (4 / WAVES) + wave / WAVES;         // this wavefront's row of the tile
         if (parts <= 1) continue;                                      // (uniform over the workgroup: so is every barrier below)
         const bool on = c < r.rows;
         const int row = r.row0 + min(c, r.rows - 1), query = row / a.group;
         const int64_t orow = r.first + query;
         const int h = head * a.group + row - query * a.group;
-        const int64_t at = (orow * a.sh.q_heads + h) * a.splits;
-        const f32x4* const po = reinterpret_cast<const f32x4*>(a.part_o + at * D) + d;
+        const int64_t at = kv4_part<MANY>(a, b, head, row, orow, h);
+        const f32x4* const po = reinterpret_cast<const f32x4*>(plan.part_o + at * D) + d;
         float top = -__builtin_inff();
-        for (int s = lane; s < parts; s += 64) top = __builtin_fmaxf(top, a.part_ml[at + s].x);
+        for (int s = lane; s < parts; s += 64) top = __builtin_fmaxf(top, plan.part_ml[at + s].x);
         top = wave_max(top);
         f32x4 sum = {0.f, 0.f, 0.f, 0.f};
         float weights = 0.f;
         for (int s0 = 0; s0 < parts; s0 += 64) {
             float f = 0.f;
             if (s0 + lane < parts) {
-                const float2 ml = a.part_ml[at + s0 + lane];
+                const float2 ml = plan.part_ml[at + s0 + lane];
                 f = ml.x > -__builtin_inff() ? exp2_fast(ml.x - top) : 0.f;
                 weights += f * ml.y;
             }
@@ -380,15 +386,38 @@ __global__ __launch_bounds__(256) void kv4_join_kernel(Kv4Args a) {
     }
 }
 
+// a workgroup to a row where it may have many parts, a wavefront otherwise
+template <int D, bool MANY>
+hipError_t join(const Kv4Args& a, hipStream_t s) {
+    const Kv4Plan& plan = MANY ? a.many : a.few;
+    const unsigned rows = MANY ? kManyRows : 16;
+    const dim3 grid((unsigned)(plan.row_tiles * a.sh.kv_heads), plan.splits > 8 ? rows : rows / 4, (unsigned)a.sh.n_requests);
+    if (plan.splits > 8) hipLaunchKernelGGL((kv4_join_kernel<D, 4, MANY>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((kv4_join_kernel<D, 1, MANY>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
 template <int D>
 hipError_t launch_d(const Kv4Args& a, hipStream_t s) {
-    const unsigned y = (unsigned)(a.row_tiles * a.sh.kv_heads);
-    hipLaunchKernelGGL((kv4_few_kernel<D>), dim3((unsigned)a.splits, y, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.splits == 1) return e;
-    // a workgroup to a row where it has many parts, or there are few rows; a wavefront otherwise
-    if (a.splits > 8) hipLaunchKernelGGL((kv4_join_kernel<D, 4>), dim3(y, 16, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((kv4_join_kernel<D, 1>), dim3(y, 4, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
-    return hipGetLastError();
+    if (a.many.run) {
+        hipError_t e = launch_kv4_many(a, s);
+        if (e == hipSuccess && a.many.splits > 1) e = join<D, true>(a, s);
+        if (e != hipSuccess) return e;
+    }
+    if (!a.few.run) return hipSuccess;
+    const unsigned y = (unsigned)(a.few.row_tiles * a.sh.kv_heads);
+    hipLaunchKernelGGL((kv4_few_kernel<D>), dim3((unsigned)a.few.splits, y, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess || a.few.splits == 1) return e;
+    return join<D, false>(a, s);
+}
+
+// The cached tokens of `lots` tiles cut into parts: `least` tokens at least, and no more than give `wanted` workgroups, all at work at once.
+void cut(Kv4Plan& p, int64_t seen, int64_t lots, int64_t least, int64_t wanted) {
+    int64_t chunk = (seen * lots / wanted + least - 1) / least * least;
+    if (chunk < least) chunk = least;
+    if (chunk > (1 << 30)) chunk = 1 << 30;
+    p.chunk = (int)chunk;
+    p.splits = (int)((seen + chunk - 1) / chunk);
 }
 
 }  // namespace
@@ -408,32 +437,38 @@ size_t plan_kv4(Kv4Args& a, void* workspace) {
     const lqer_kv4_shape& sh = a.sh;
     a.group = sh.q_heads / sh.kv_heads;
     a.P_bits = __builtin_ctz((unsigned)sh.page_tokens);
-    const int64_t rows = (int64_t)sh.max_q * a.group;
-    int64_t tiles = (rows + 15) / 16;
-    const int64_t most_tiles = 65535 / sh.kv_heads;
-    a.row_tiles = (int)(tiles < 1 ? 1 : tiles > most_tiles ? most_tiles : tiles);
-    // Parts of the axis: 128 tokens at least (a step of 32 for each wavefront), and about three workgroups to a compute unit, all at work at once
-    int64_t seen = sh.max_kv;
-    if (sh.window > 0 && (int64_t)sh.window + sh.max_q + 31 < seen) seen = (int64_t)sh.window + sh.max_q + 31;
-    if (seen < 1) seen = 1;
-    const int64_t lots = (int64_t)sh.n_requests * sh.kv_heads * a.row_tiles;
-    int64_t chunk = (seen * lots / 768 + 127) / 128 * 128;
-    if (chunk < 128) chunk = 128;
-    if (chunk > (1 << 30)) chunk = 1 << 30;
-    int64_t splits = (seen + chunk - 1) / chunk;
-    // (what the parts write and the join reads is bounded: the parts' sums are fp32)
-    while (splits > 1 && splits * sh.Tq * sh.q_heads * sh.head_dim * 4 > ((int64_t)256 << 20)) splits = (splits + 1) / 2;
-    a.chunk = (int)chunk;
-    a.splits = (int)splits;
-    if (splits == 1) {
-        a.part_o = nullptr;
-        a.part_ml = nullptr;
-        return 0;
-    }
-    const int64_t n = splits * sh.Tq * sh.q_heads;
-    a.part_o = (float*)workspace;
-    a.part_ml = (float2*)((uint8_t*)workspace + n * sh.head_dim * 4);
-    return (size_t)(n * (sh.head_dim * 4 + 8));
+    a.few_rows = kFewRows;
+    const int64_t rows = (int64_t)sh.max_q * a.group, most_tiles = 65535 / sh.kv_heads;
+    const auto tiles = [&](int64_t n, int64_t of) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + of - 1) / of, most_tiles)); };
+    // Requests of few rows beside ones of many: only where some are shorter than the longest.
+    a.many = Kv4Plan{};
+    a.few = Kv4Plan{};
+    a.many.run = rows > kFewRows;
+    a.few.run = !a.many.run || sh.Tq < (int64_t)sh.n_requests * sh.max_q;
+    a.many.row_tiles = tiles(rows, kManyRows);
+    a.few.cap = (int)std::max<int64_t>(1, std::min<int64_t>(rows, kFewRows));
+    a.few.row_tiles = tiles(a.few.cap, 16);
+    int64_t seen = std::max(sh.max_kv, 1);
+    if (sh.window > 0) seen = std::min<int64_t>(seen, (int64_t)sh.window + sh.max_q + 31);
+    const int64_t heads = (int64_t)sh.n_requests * sh.kv_heads;
+    // 128 tokens are a step of 32 for each wavefront of a workgroup, 512 are eight steps of a workgroup for many rows: those keep two
+    // workgroups to a compute unit, the others three
+    cut(a.few, seen, heads * a.few.row_tiles, 128, 768);
+    cut(a.many, seen, heads * a.many.row_tiles, 512, 512);
+    size_t at = 0;
+    const auto place = [&](Kv4Plan& p, int64_t n) {
+        if (!p.run) return;
+        // (what the parts write and the join reads is bounded: the parts' sums are fp32)
+        while (p.splits > 1 && p.splits * n * sh.head_dim * 4 > ((int64_t)256 << 20)) p.splits = (p.splits + 1) / 2;
+        if (p.splits == 1) return;
+        n *= p.splits;
+        p.part_o = (float*)((uint8_t*)workspace + at);
+        p.part_ml = (float2*)((uint8_t*)workspace + at + n * sh.head_dim * 4);
+        at += (size_t)(n * (sh.head_dim * 4 + 8) + 255) / 256 * 256;
+    };
+    place(a.few, heads * a.few.cap);
+    place(a.many, sh.Tq * sh.q_heads);
+    return at;
 }
 
 hipError_t launch_kv4_attention(const Kv4Args& a, hipStream_t s) {

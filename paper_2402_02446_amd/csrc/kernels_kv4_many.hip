@@ -1,0 +1,283 @@
+// Attention of many query rows over the MXINT4 cache: prompts, and chunks of them.
+//
+// Bound by the matrix instructions and the exponentials beside them.  A workgroup has 128 rows (query, head of the group) of one cached head,
+// 32 to each of its four wavefronts, and takes the cached tokens in tiles of 64 (32 at D = 256).  All four turn a tile's words into bf16
+// once, a lane 16 bytes of a key and a cell of four tokens by eight dimensions of values, and store them in LDS as the operands of the
+// 32 x 32 x 16 matrix instruction in the order in which the wavefronts read them, 64 lanes x 16 bytes; two tiles' room, so that
+// one barrier a tile is enough, and the next tile's words are loaded meanwhile.
+//   S^T = K Q^T      tokens as rows, query rows as columns: a lane holds half of the tokens of one row, the lane 32 further the others
+//   O^T += V^T P^T   the scores' registers are the operand as they are (tokens in the order in which the lanes hold them)
+// The running maximum is moved only when a score passes it by more than 2^8: until then the weights, relative to the older
+// maximum, are at most 2^8, which costs no precision, and the accumulators need no rescaling.  The weights enter the product as bf16
+// (relative 2^-8 at most), their sum in fp32.
+#include "kv4_device.h"
+
+namespace lqer {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+template <int D>
+struct Tile {
+    static constexpr int TOKENS = D == 256 ? 32 : 64;
+    static constexpr int KEYS = TOKENS * D * 2;                    // bytes of a tile's keys in LDS; as many of its values
+    static constexpr int K_THREADS = TOKENS * D / 32;              // 16 bytes (32 dimensions) of a key each: 256, at D = 64 128
+    static constexpr int E = 256 / D;                              // dimensions of a word that share a tile of 32 output dimensions
+};
+
+// A thread's words of a tile, on their way: 32 dimensions of a key, and a cell of values.  At D = 64 the first two wavefronts have the
+// keys and the others the values.
+struct Words {
+    u32x4 k, v;
+    uint32_t ke, ve;
+};
+
+template <int D>
+__device__ __forceinline__ Words load_words(const Kv4Args& a, const Kv4Record<D> R, const int32_t* table, int head, int t0, int from, int end) {
+    using T = Tile<D>;
+    Words w{};
+    const auto record = [&](int t, bool& there) {
+        const int index = t >> a.P_bits;
+        const int page = t < end && index < a.sh.table_ld ? table[index] : -1;
+        there = page >= 0 && page < a.sh.pages;
+        return a.pool + ((int64_t)(there ? page : 0) * a.sh.kv_heads + head) * R.bytes();
+    };
+    const int mask = (1 << a.P_bits) - 1, tid = threadIdx.x;
+    if (tid < T::K_THREADS) {
+        const int t = t0 + tid % T::TOKENS, c = tid / T::TOKENS;
+        bool there;
+        const uint8_t* rec = record(t, there);
+        if (there) {
+            w.k = *reinterpret_cast<const u32x4*>(rec + R.key(t & mask) + 16 * c);
+            w.ke = *reinterpret_cast<const uint16_t*>(rec + R.key_exp(t & mask) + 2 * c);
+        }
+    }
+    const int cell = D == 64 ? tid - 128 : tid;
+    if (cell >= 0) {
+        const int word = cell % (D / 8), t = t0 + cell / (D / 8) * 4;
+        bool there;
+        const uint8_t* rec = record(t, there);
+        if (there) {
+            w.v = *reinterpret_cast<const u32x4*>(rec + R.value((t & mask) / 4) + word * 16);
+            w.ve = *reinterpret_cast<const uint32_t*>(rec + R.value_exp((t & mask) / 4) + word / 2 * 4);
+            // tokens that no row sees may hold anything: their weights are 0, and meet a finite number
+            const int before = from - t, n = end - t;
+            if (before > 0) w.ve = before < 4 ? w.ve >> (8 * before) << (8 * before) : 0u;
+            if (n < 4) w.ve &= (1u << (8 * n)) - 1u;
+        }
+    }
+    return w;
+}
+
+// ... and into LDS as operands.  Keys: [32 tokens][step of 16 dimensions][64 lanes][16 B]; values: [tile of 32 output dimensions][step of 16
+// tokens][64 lanes][16 B], output dimension 8 w + e being row E w + e % E of tile e / E.
+template <int D>
+__device__ __forceinline__ void store_words(const Words& w, uint8_t* keys, uint8_t* values) {
+    using T = Tile<D>;
+    const int tid = threadIdx.x;
+    if (tid < T::K_THREADS) {
+        const int t = tid % T::TOKENS, c = tid / T::TOKENS;
+        uint8_t* const at = keys + (t / 32) * (32 * D * 2) + (t & 31) * 16;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            Frag f;
+            f.v = unpack_w8(w.k[j], kv4_scale((w.ke >> (8 * (j / 2))) & 0xFFu));
+            const int word = 4 * c + j;
+            *reinterpret_cast<u32x4*>(at + ((word >> 1) * 64 + (word & 1) * 32) * 16) = f.u;
+        }
+    }
+    const int cell = D == 64 ? tid - 128 : tid;
+    if (cell >= 0) {
+        const int word = cell % (D / 8), four = cell / (D / 8);    // four: which four tokens
+        uint32_t t[4][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            Frag f;
+            f.v = unpack_w8(w.v[j], kv4_scale((w.ve >> (8 * j)) & 0xFFu));
+#pragma unroll
+            for (int x = 0; x < 4; ++x) t[j][x] = f.u[x];
+        }
+        // tokens 16 s + 4 hh .. and 16 s + 8 + 4 hh ..: the two halves of lane half hh
+        uint8_t* const at = values + ((four >> 2) * 64 + (four & 1) * 32 + T::E * word) * 16 + ((four >> 1) & 1) * 8;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
+            const u32x2 half = {__builtin_amdgcn_perm(t[1][e / 2], t[0][e / 2], sel), __builtin_amdgcn_perm(t[3][e / 2], t[2][e / 2], sel)};
+            *reinterpret_cast<u32x2*>(at + ((e / T::E) * (T::TOKENS / 16) * 64 + e % T::E) * 16) = half;
+        }
+    }
+}
+
+__device__ __forceinline__ float halves_max(float v) {
+    const auto b = __builtin_amdgcn_permlane32_swap(f32_bits(v), f32_bits(v), false, false);
+    return __builtin_fmaxf(f32_from_bits(b[0]), f32_from_bits(b[1]));
+}
+
+template <int D>
+__global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args a) {
+    using T = Tile<D>;
+    constexpr int QS = D / 16, NO = D / 32, U = T::TOKENS / 32;
+    __shared__ __align__(16) uint8_t keys[2][T::KEYS];
+    __shared__ __align__(16) uint8_t values[2][T::KEYS];
+    __shared__ uint32_t absent[2][2];              // bits of a tile's tokens whose page is none of the pool's
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, hh = lane >> 5;
+    const int head = blockIdx.y % a.sh.kv_heads, b = blockIdx.z, split = blockIdx.x;
+    Kv4Rows r = kv4_request(a, b);
+    if (!kv4_mine<true>(a, r)) return;
+    const Kv4Record<D> R{a.P_bits};
+    const int32_t* const table = a.table + (int64_t)b * a.sh.table_ld;
+    const float to_log2 = __builtin_fmaxf(__builtin_fabsf(a.sh.scale) * kLog2e, 0x1p-126f);      // as for few rows
+    const uint32_t turn = a.sh.scale < 0.f ? 0x80008000u : 0u;
+    const int all_rows = r.n * a.group, tiles = (all_rows + kManyRows - 1) / kManyRows;
+    // (the last rows see the most tokens of a causal prompt: they start first)
+    for (int tile = tiles - 1 - (int)(blockIdx.y / a.sh.kv_heads); tile >= 0; tile -= a.many.row_tiles) {
+        kv4_tile(a, r, tile * kManyRows, kManyRows);
+        int chunk;
+        const int parts = kv4_parts<true>(a, r, chunk);
+        if (split >= parts && split > 0) continue;
+        const int lo = (r.lo & ~31) + split * chunk, hi = min(r.hi, lo + chunk);
+        // this wavefront's rows, this lane's
+        const int w_first = min(r.row0 + 32 * wave, r.row0 + r.rows - 1), w_last = min(w_first + 31, r.row0 + r.rows - 1);
+        const bool idle = 32 * wave >= r.rows;
+        const int row = min(r.row0 + 32 * wave + i, r.row0 + r.rows - 1), query = row / a.group;
+        const int64_t orow = r.first + query;
+        const int h = head * a.group + row - query * a.group;
+        const int begin = kv4_row_begin(a, r, query), end = kv4_row_end(a, r, query);
+        const int w_begin = kv4_row_begin(a, r, w_first / a.group), w_end = idle ? 0 : kv4_row_end(a, r, w_last / a.group);
+        const int all_begin = kv4_row_begin(a, r, w_last / a.group), all_end = kv4_row_end(a, r, w_first / a.group);
+        Frag q[QS];
+        {
+            const uint16_t* p = a.q + orow * a.sh.ldq + (int64_t)h * D + 8 * hh;
+#pragma unroll
+            for (int s = 0; s < QS; ++s) q[s].u = *reinterpret_cast<const u32x4*>(p + 16 * s) ^ turn;
+        }
+        f32x16 o[NO];
+#pragma unroll
+        for (int x = 0; x < NO; ++x)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) o[x][j] = 0.f;
+        float m = -__builtin_inff(), l = 0.f;
+        Words words = load_words<D>(a, R, table, head, lo, r.lo, hi);
+        int buf = 0;
+        for (int t0 = lo; t0 < hi; t0 += T::TOKENS, buf ^= 1) {
+            store_words<D>(words, keys[buf], values[buf]);
+            if (wave == 0) {
+                const int t = t0 + lane, index = t >> a.P_bits;
+                const int page = t < hi && index < a.sh.table_ld ? table[index] : 0;
+                const uint64_t none = __ballot(page < 0 || page >= a.sh.pages);
+                if (lane == 0) {
+                    absent[buf][0] = (uint32_t)none;
+                    absent[buf][1] = (uint32_t)(none >> 32);
+                }
+            }
+            if (t0 + T::TOKENS < hi) words = load_words<D>(a, R, table, head, t0 + T::TOKENS, r.lo, hi);
+            __syncthreads();
+            if (t0 >= w_end || t0 + T::TOKENS <= w_begin) continue;      // nothing that this wavefront's rows see
+            f32x16 s[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[u][j] = 0.f;
+#pragma unroll
+                for (int x = 0; x < QS; ++x) {
+                    Frag f;
+                    f.u = *reinterpret_cast<const u32x4*>(keys[buf] + u * (32 * D * 2) + (x * 64 + lane) * 16);
+                    s[u] = mfma32(f.v, q[x].v, s[u]);
+                }
+            }
+            const uint32_t none = absent[buf][0] | absent[buf][1];
+            if (t0 < all_begin || t0 + T::TOKENS > all_end || t0 + T::TOKENS > hi || __builtin_amdgcn_readfirstlane(none) != 0) {
+                int at = t0;
+                asm volatile("" : "+s"(at));       // (a branch: left alone, the comparisons are done for every tile)
+                const int stop = min(end, hi);
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int j = 0; j < 16; ++j) {
+                        const int k = 8 * (j >> 2) + 4 * hh + (j & 3), t = at + 32 * u + k;
+                        if (t >= stop || t < begin || ((absent[buf][u] >> k) & 1u)) s[u][j] = -__builtin_inff();
+                    }
+            }
+            float top = s[0][0];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) top = __builtin_fmaxf(top, s[u][j]);
+            top = halves_max(top) * to_log2;
+            if (__ballot(top > m + 8.0f)) {        // (also the first score: m is minus infinity)
+                const float next = __builtin_fmaxf(m, top), down = m == -__builtin_inff() ? 0.f : exp2_fast(m - next);
+                l *= down;
+#pragma unroll
+                for (int x = 0; x < NO; ++x) o[x] *= down;
+                m = next;
+            }
+            const float base = m == -__builtin_inff() ? 0.f : m;
+            Frag p[2 * U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+#pragma unroll
+                for (int j = 0; j < 16; j += 2) {
+                    const float e0 = exp2_fast(__builtin_fmaf(s[u][j], to_log2, -base));
+                    const float e1 = exp2_fast(__builtin_fmaf(s[u][j + 1], to_log2, -base));
+                    l += e0;
+                    l += e1;
+                    p[2 * u + (j >> 3)].u[(j >> 1) & 3] = pack_bf16_near(e0, e1);
+                }
+#pragma unroll
+            for (int k = 0; k < 2 * U; ++k)
+#pragma unroll
+                for (int x = 0; x < NO; ++x) {
+                    Frag f;
+                    f.u = *reinterpret_cast<const u32x4*>(values[buf] + ((x * (2 * U) + k) * 64 + lane) * 16);
+                    o[x] = mfma32(f.v, p[k].v, o[x]);
+                }
+        }
+        __syncthreads();                           // (the next tile of rows stores into LDS from its beginning)
+        {
+            const auto both = __builtin_amdgcn_permlane32_swap(f32_bits(l), f32_bits(l), false, false);
+            l = f32_from_bits(both[0]) + f32_from_bits(both[1]);
+        }
+        if (32 * wave + i >= r.rows) continue;
+        const float by = parts > 1 ? 1.0f : l > 0.f ? 1.0f / l : 0.f;
+        const int64_t part = parts > 1 ? kv4_part<true>(a, b, head, row, orow, h) + split : 0;
+        if (parts > 1 && hh == 0) a.many.part_ml[part] = float2{m, l};
+        // rows of the output tiles: register j of lane half hh is row 8 (j / 4) + 4 hh + j % 4; eight neighbouring dimensions lie in E
+        // registers of every tile
+#pragma unroll
+        for (int j = 0; j < 16; j += T::E) {
+            const int row_of = 8 * (j >> 2) + 4 * hh + (j & 3), word = row_of / T::E;
+            float v[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = o[e / T::E][j + e % T::E] * by;
+            if (parts > 1) {
+                f32x4* p = reinterpret_cast<f32x4*>(a.many.part_o + part * D + 8 * word);
+                p[0] = f32x4{v[0], v[1], v[2], v[3]};
+                p[1] = f32x4{v[4], v[5], v[6], v[7]};
+            } else if (a.sh.out_type == LQER_F32) {
+                f32x4* p = reinterpret_cast<f32x4*>((float*)a.out + orow * a.sh.ldo + (int64_t)h * D + 8 * word);
+                p[0] = f32x4{v[0], v[1], v[2], v[3]};
+                p[1] = f32x4{v[4], v[5], v[6], v[7]};
+            } else {
+                *reinterpret_cast<u32x4*>((uint16_t*)a.out + orow * a.sh.ldo + (int64_t)h * D + 8 * word) =
+                    u32x4{pack_bf16_near(v[0], v[1]), pack_bf16_near(v[2], v[3]), pack_bf16_near(v[4], v[5]), pack_bf16_near(v[6], v[7])};
+            }
+        }
+    }
+}
+
+template <int D>
+hipError_t launch_d(const Kv4Args& a, hipStream_t s) {
+    const dim3 grid((unsigned)a.many.splits, (unsigned)(a.many.row_tiles * a.sh.kv_heads), (unsigned)a.sh.n_requests);
+    hipLaunchKernelGGL((kv4_many_kernel<D>), grid, dim3(256), 0, s, a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_kv4_many(const Kv4Args& a, hipStream_t s) {
+    if (a.sh.head_dim == 64) return launch_d<64>(a, s);
+    return a.sh.head_dim == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
+}
+
+}  // namespace lqer

@@ -53,13 +53,33 @@ __device__ __forceinline__ void kv4_tile(const Kv4Args& a, Kv4Rows& r, int row0,
     if (r.hi < r.lo) r.hi = r.lo;
 }
 
+// Whether this request is the business of the kernel for many rows (MANY) or of the other one.
+template <bool MANY>
+__device__ __forceinline__ bool kv4_mine(const Kv4Args& a, const Kv4Rows& r) {
+    if (MANY) return !a.few.run || (int64_t)r.n * a.group > a.few_rows;
+    return !a.many.run || (int64_t)r.n * a.group <= a.few_rows;
+}
+
 // The parts that a tile's tokens are cut into: their length and number.  Parts begin at multiples of 32 tokens.
+template <bool MANY>
 __device__ __forceinline__ int kv4_parts(const Kv4Args& a, const Kv4Rows& r, int& chunk) {
+    const Kv4Plan& plan = MANY ? a.many : a.few;
     const int lo = r.lo & ~31, all = r.hi > r.lo ? r.hi - lo : 0;
-    chunk = a.chunk;
-    const int least = (all + a.splits - 1) / a.splits;
+    if (!MANY && r.row0 + r.rows > plan.cap) {         // rows beyond the estimate: no room for their parts
+        chunk = (all + 31) & ~31;
+        return all > 0 ? 1 : 0;
+    }
+    chunk = plan.chunk;
+    const int least = (all + plan.splits - 1) / plan.splits;
     if (least > chunk) chunk = (least + 31) & ~31;
     return (all + chunk - 1) / chunk;
+}
+
+// Where the parts of a row (query row orow, query head h; row of request b and cached head) lie.
+template <bool MANY>
+__device__ __forceinline__ int64_t kv4_part(const Kv4Args& a, int b, int head, int row, int64_t orow, int h) {
+    if (MANY) return (orow * a.sh.q_heads + h) * a.many.splits;
+    return (((int64_t)b * a.sh.kv_heads + head) * a.few.cap + row) * a.few.splits;
 }
 
 // fp32 scale 2^(eb - 127 - 2 + 9) of a block of the cache (w_scale of the weights): the byte is at most 247.

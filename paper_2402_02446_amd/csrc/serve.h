@@ -68,6 +68,19 @@ struct Kv4AppendArgs {
 };
 hipError_t launch_kv4_append(const Kv4AppendArgs& a, hipStream_t s);
 
+constexpr int kFewRows = 64;           // query rows (query, head of the group) that the kernel for few rows takes, in tiles of 16
+constexpr int kManyRows = 128;         // rows of a workgroup of the kernel for many
+
+// How one of the two kernels is laid out: tiles of query rows (query, head of the group) and parts of the cached tokens.
+struct Kv4Plan {
+    bool run;
+    int row_tiles;         // tiles of rows of a request that have workgroups of their own
+    int chunk;             // cached tokens of a part, at least
+    int splits;            // most parts
+    int cap;               // few rows: the rows of a request and cached head that have room for their parts
+    float* part_o;         // [..][splits][D]: a part's sum of weighted values,
+    float2* part_ml;       // [..][splits]: its maximum (in units of log 2) and sum of weights; [n_requests][kv_heads][cap] or [Tq][q_heads]
+};
 struct Kv4Args {
     lqer_kv4_shape sh;
     const uint8_t* pool;
@@ -79,13 +92,11 @@ struct Kv4Args {
     // set by plan_kv4
     int group;             // query heads of a cached head
     int P_bits;
-    int row_tiles;         // tiles of query rows (query, head of the group) a request's launch is laid out for
-    int chunk;             // cached tokens of one part of the axis, at least
-    int splits;            // most parts
-    float* part_o;         // [Tq][q_heads][splits][D]: a part's sum of weighted values,
-    float2* part_ml;       // [Tq][q_heads][splits]: its maximum (in units of log 2) and sum of weights
+    int few_rows;          // requests of up to so many rows go to the kernel for few, where both run
+    Kv4Plan few, many;
 };
 size_t plan_kv4(Kv4Args& a, void* workspace);
 hipError_t launch_kv4_attention(const Kv4Args& a, hipStream_t s);
+hipError_t launch_kv4_many(const Kv4Args& a, hipStream_t s);          // kernels_kv4_many.hip
 
 }  // namespace lqer

@@ -4,7 +4,9 @@ Appending: the pool's bytes are the oracle's, and no other byte changes.
 Attention, tolerance derived: keys, values and queries enter exactly (codes times powers of two, bf16); scores are fp32; the weights enter the
 product with V as two bf16 terms (relative 2^-16); the exponentials and the fp32 scores behind them (arguments of up to about 100, relative 2^-24
 times a few) add at most 2^-12; a bf16 output is rounded by 2^-8 of itself at most, and |o| <= sum_t w_t |V_t|.  Elementwise, within
-|error| <= (2^-9 + 2^-12) sum_t w_t |V_t| + 2^-9 |o| (the last term for bf16 outputs), w the exact weights."""
+|error| <= (2^-9 + 2^-12) sum_t w_t |V_t| + 2^-9 |o| (the last term for bf16 outputs), w the exact weights.
+Where a request has more than 64 rows (queries times heads of a group) the weights enter as one bf16 term, rounded by 2^-8 at most, their sum in
+fp32: |error| <= (2^-8 + 2^-12) sum_t w_t |V_t| + 2^-8 |o|."""
 import numpy as np
 import pytest
 
@@ -68,7 +70,8 @@ def _attend(q_lens, lens, q_heads, kv_heads, D, P, causal=True, window=0, scale=
         for h in range(q_heads):
             qq = q[cu[b]: cu[b + 1], h].double().numpy()
             o, mag = block.attention(qq, K[b][:t, h // G], V[b][:t, h // G], scale, begin, end, seen[b])
-            bound = (2.0 ** -9 + 2.0 ** -12) * mag + (0 if f32 else 2.0 ** -9) * np.abs(o)
+            unit = 2.0 ** -8 if n * G > 64 else 2.0 ** -9
+            bound = (unit + 2.0 ** -12) * mag + (0 if f32 else unit) * np.abs(o)
             err = np.abs(got[cu[b]: cu[b + 1], h] - o)
             assert np.all(err <= bound), (b, h, np.argwhere(~(err <= bound))[:3].tolist(), float(np.nanmax(err)))
     assert np.all(got[cu[-1]:] == 7.0)
@@ -152,11 +155,37 @@ def test_long_and_split():
     _attend([1, 0, 1], [3000, 0, 1], 4, 1, 256, 128, f32=True)
 
 
-# ---- several tokens -------------------------------------------------------------------------------------------------------
+# ---- several tokens: tiles of 16 and of 128 rows, requests of either kind in one call -------------------------------------------------------------------------------------------------------
 @pytest.mark.parametrize("D", [64, 128, 256])
 @pytest.mark.parametrize("q_len", [2, 5, 17, 40])
 def test_several_tokens(D, q_len):
     _attend([q_len, 1, 0, q_len - 1], [q_len, 150, 9, 77], 6, 2, D, 16)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("q_heads, kv_heads", [(1, 1), (3, 1), (8, 2), (40, 1)])
+def test_prompts(D, q_heads, kv_heads):
+    _attend([130, 33, 64], [130, 200, 64], q_heads, kv_heads, D, 32)
+
+
+@pytest.mark.parametrize("length", [33, 63, 64, 65, 95, 96, 97, 127, 128, 129, 191, 193, 257])
+def test_prompt_lengths(length):
+    _attend([length, 40], [length, length], 1, 1, 128, 16)
+    _attend([length], [length + 70], 1, 1, 64, 64, f32=True)
+    _attend([length], [length + 3], 1, 1, 256, 16)
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_a_chunk_on_a_long_cache(D):
+    """Few tiles of rows over many tokens: the axis is cut into parts."""
+    _attend([20], [3000], 4, 2, D, 64)
+    _attend([40, 35], [1500, 2100], 2, 1, D, 16, f32=True, window=900)
+
+
+def test_prompts_and_single_tokens_in_one_call():
+    _attend([1, 200, 1, 3, 0, 33], [900, 260, 1, 70, 0, 400], 8, 2, 128, 16)
+    _attend([300, 1, 1], [300, 2500, 700], 4, 1, 64, 64, f32=True)
+    _attend([5, 100, 8, 9], [50, 100, 64, 300], 4, 1, 256, 16, causal=False)
 
 
 @pytest.mark.parametrize("window", [1, 2, 16, 33, 100, 1000])
