@@ -2,7 +2,7 @@
 //
 // Bound by the matrix instructions and the exponentials beside them.  A workgroup has 128 rows (query, head of the group) of one cached head,
 // 32 to each of its four wavefronts, and takes the cached tokens in tiles of 64 (32 at D = 256).  All four turn a tile's words into bf16
-// once, a lane 16 bytes of a key and a cell of four tokens by eight dimensions of values, and store them in LDS as the operands of the
+// once, a lane 16 bytes of a key and a cell of four tokens by eight dimensions of values, a wavefront 16 tokens, and store them in LDS as the operands of the
 // 32 x 32 x 16 matrix instruction in the order in which the wavefronts read them, 64 lanes x 16 bytes; two tiles' room, so that
 // one barrier a tile is enough, and the next tile's words are loaded meanwhile.
 //   S^T = K Q^T      tokens as rows, query rows as columns: a lane holds half of the tokens of one row, the lane 32 further the others
@@ -22,50 +22,53 @@ template <int D>
 struct Tile {
     static constexpr int TOKENS = D == 256 ? 32 : 64;
     static constexpr int KEYS = TOKENS * D * 2;                    // bytes of a tile's keys in LDS; as many of its values
-    static constexpr int K_THREADS = TOKENS * D / 32;              // 16 bytes (32 dimensions) of a key each: 256, at D = 64 128
     static constexpr int E = 256 / D;                              // dimensions of a word that share a tile of 32 output dimensions
 };
 
-// A thread's words of a tile, on their way: 32 dimensions of a key, and a cell of values.  At D = 64 the first two wavefronts have the
-// keys and the others the values.
+// A lane's words of a tile, on their way: 32 dimensions of a key, and a cell of values.  A wavefront's are those of the same 16 tokens, which
+// lie in one page: its number is a scalar.  At D = 64 the first 32 lanes have the keys and the others the values.
 struct Words {
     u32x4 k, v;
     uint32_t ke, ve;
 };
-
 template <int D>
-__device__ __forceinline__ Words load_words(const Kv4Args& a, const Kv4Record<D> R, const int32_t* table, int head, int t0, int from, int end) {
-    using T = Tile<D>;
-    Words w{};
-    const auto record = [&](int t, bool& there) {
-        const int index = t >> a.P_bits;
-        const int page = t < end && index < a.sh.table_ld ? table[index] : -1;
-        there = page >= 0 && page < a.sh.pages;
-        return a.pool + ((int64_t)(there ? page : 0) * a.sh.kv_heads + head) * R.bytes();
-    };
-    const int mask = (1 << a.P_bits) - 1, tid = threadIdx.x;
-    if (tid < T::K_THREADS) {
-        const int t = t0 + tid % T::TOKENS, c = tid / T::TOKENS;
-        bool there;
-        const uint8_t* rec = record(t, there);
-        if (there) {
-            w.k = *reinterpret_cast<const u32x4*>(rec + R.key(t & mask) + 16 * c);
-            w.ke = *reinterpret_cast<const uint16_t*>(rec + R.key_exp(t & mask) + 2 * c);
-        }
+struct Part {
+    int sub;               // which 16 tokens of the tile
+    int t, c;              // key: token of the 16, which 32 dimensions
+    int four, word;        // values: which four tokens of the 16, word of eight dimensions
+    bool k, v;
+    __device__ __forceinline__ Part(int wave, int lane) {
+        sub = D == 256 ? wave >> 1 : wave;
+        t = lane & 15;
+        c = D == 64 ? (lane >> 4) & 1 : D == 128 ? lane >> 4 : (lane >> 4) + 4 * (wave & 1);
+        const int cell = D == 64 ? lane & 31 : lane;
+        four = D == 256 ? cell >> 4 : cell / (D / 8);
+        word = D == 256 ? (cell & 15) + 16 * (wave & 1) : cell % (D / 8);
+        k = D != 64 || lane < 32;
+        v = D != 64 || lane >= 32;
     }
-    const int cell = D == 64 ? tid - 128 : tid;
-    if (cell >= 0) {
-        const int word = cell % (D / 8), t = t0 + cell / (D / 8) * 4;
-        bool there;
-        const uint8_t* rec = record(t, there);
-        if (there) {
-            w.v = *reinterpret_cast<const u32x4*>(rec + R.value((t & mask) / 4) + word * 16);
-            w.ve = *reinterpret_cast<const uint32_t*>(rec + R.value_exp((t & mask) / 4) + word / 2 * 4);
-            // tokens that no row sees may hold anything: their weights are 0, and meet a finite number
-            const int before = from - t, n = end - t;
-            if (before > 0) w.ve = before < 4 ? w.ve >> (8 * before) << (8 * before) : 0u;
-            if (n < 4) w.ve &= (1u << (8 * n)) - 1u;
-        }
+};
+
+// page: of the wavefront's 16 tokens, -1 where they are not there.  [from, end): what the workgroup's rows see of the part.
+template <int D>
+__device__ __forceinline__ Words load_words(const Kv4Args& a, const Kv4Record<D> R, const Part<D>& part, int page, int head, int t0, int from, int end) {
+    Words w{};
+    if (page < 0) return w;
+    const int t = t0 + 16 * part.sub, off = t & ((1 << a.P_bits) - 1);
+    const uint8_t* const rec = a.pool + ((int64_t)page * a.sh.kv_heads + head) * R.bytes();
+    if (part.k) {
+        w.k = *reinterpret_cast<const u32x4*>(rec + R.key(off) + (uint32_t)(part.t * (D / 2) + 16 * part.c));
+        w.ke = *reinterpret_cast<const uint16_t*>(rec + R.key_exp(off) + (uint32_t)(part.t * (D / 16) + 2 * part.c));
+    }
+    if (part.v) {
+        w.v = *reinterpret_cast<const u32x4*>(rec + R.value(off / 4) + (uint32_t)(part.four * (2 * D) + part.word * 16));
+        w.ve = *reinterpret_cast<const uint32_t*>(rec + R.value_exp(off / 4) + (uint32_t)(part.four * (D / 4) + part.word / 2 * 4));
+    }
+    if (t < from || t + 16 > end) {
+        // tokens that no row sees may hold anything: their weights are 0, and meet a finite number
+        const int before = from - (t + 4 * part.four), n = end - (t + 4 * part.four);
+        if (before > 0) w.ve = before < 4 ? w.ve >> (8 * before) << (8 * before) : 0u;
+        if (n < 4) w.ve = n > 0 ? w.ve & ((1u << (8 * n)) - 1u) : 0u;
     }
     return w;
 }
@@ -73,23 +76,18 @@ __device__ __forceinline__ Words load_words(const Kv4Args& a, const Kv4Record<D>
 // ... and into LDS as operands.  Keys: [32 tokens][step of 16 dimensions][64 lanes][16 B]; values: [tile of 32 output dimensions][step of 16
 // tokens][64 lanes][16 B], output dimension 8 w + e being row E w + e % E of tile e / E.
 template <int D>
-__device__ __forceinline__ void store_words(const Words& w, uint8_t* keys, uint8_t* values) {
+__device__ __forceinline__ void store_words(const Words& w, const Part<D>& part, uint8_t* keys, uint8_t* values) {
     using T = Tile<D>;
-    const int tid = threadIdx.x;
-    if (tid < T::K_THREADS) {
-        const int t = tid % T::TOKENS, c = tid / T::TOKENS;
-        uint8_t* const at = keys + (t / 32) * (32 * D * 2) + (t & 31) * 16;
+    if (part.k) {
+        uint8_t* const at = keys + (part.sub / 2) * (32 * D * 2) + (4 * part.c * 32 + (part.sub & 1) * 16 + part.t) * 16;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             Frag f;
             f.v = unpack_w8(w.k[j], kv4_scale((w.ke >> (8 * (j / 2))) & 0xFFu));
-            const int word = 4 * c + j;
-            *reinterpret_cast<u32x4*>(at + ((word >> 1) * 64 + (word & 1) * 32) * 16) = f.u;
+            *reinterpret_cast<u32x4*>(at + j * 32 * 16) = f.u;
         }
     }
-    const int cell = D == 64 ? tid - 128 : tid;
-    if (cell >= 0) {
-        const int word = cell % (D / 8), four = cell / (D / 8);    // four: which four tokens
+    if (part.v) {
         uint32_t t[4][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -98,8 +96,8 @@ __device__ __forceinline__ void store_words(const Words& w, uint8_t* keys, uint8
 #pragma unroll
             for (int x = 0; x < 4; ++x) t[j][x] = f.u[x];
         }
-        // tokens 16 s + 4 hh .. and 16 s + 8 + 4 hh ..: the two halves of lane half hh
-        uint8_t* const at = values + ((four >> 2) * 64 + (four & 1) * 32 + T::E * word) * 16 + ((four >> 1) & 1) * 8;
+        // tokens 4 hh .. and 8 + 4 hh .. of the 16: the two halves of lane half hh
+        uint8_t* const at = values + (part.sub * 64 + (part.four & 1) * 32 + T::E * part.word) * 16 + (part.four >> 1) * 8;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
@@ -120,12 +118,13 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
     constexpr int QS = D / 16, NO = D / 32, U = T::TOKENS / 32;
     __shared__ __align__(16) uint8_t keys[2][T::KEYS];
     __shared__ __align__(16) uint8_t values[2][T::KEYS];
-    __shared__ uint32_t absent[2][2];              // bits of a tile's tokens whose page is none of the pool's
+    __shared__ uint32_t absent[2][4];              // whether a tile's 16 tokens have a page that is none of the pool's
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, hh = lane >> 5;
     const int head = blockIdx.y % a.sh.kv_heads, b = blockIdx.z, split = blockIdx.x;
     Kv4Rows r = kv4_request(a, b);
     if (!kv4_mine<true>(a, r)) return;
     const Kv4Record<D> R{a.P_bits};
+    const Part<D> part(wave, lane);
     const int32_t* const table = a.table + (int64_t)b * a.sh.table_ld;
     const float to_log2 = __builtin_fmaxf(__builtin_fabsf(a.sh.scale) * kLog2e, 0x1p-126f);      // as for few rows
     const uint32_t turn = a.sh.scale < 0.f ? 0x80008000u : 0u;
@@ -158,20 +157,20 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[x][j] = 0.f;
         float m = -__builtin_inff(), l = 0.f;
-        Words words = load_words<D>(a, R, table, head, lo, r.lo, hi);
+        const auto page_of = [&](int t0) {         // -1: none of the pool's
+            const int index = (t0 + 16 * part.sub) >> a.P_bits;
+            const int page = t0 < hi && index < a.sh.table_ld ? table[index] : -1;
+            return page < a.sh.pages ? page : -1;
+        };
+        int page = page_of(lo), page_next = page_of(lo + T::TOKENS);
+        Words words = load_words<D>(a, R, part, page, head, lo, r.lo, hi);
         int buf = 0;
         for (int t0 = lo; t0 < hi; t0 += T::TOKENS, buf ^= 1) {
-            store_words<D>(words, keys[buf], values[buf]);
-            if (wave == 0) {
-                const int t = t0 + lane, index = t >> a.P_bits;
-                const int page = t < hi && index < a.sh.table_ld ? table[index] : 0;
-                const uint64_t none = __ballot(page < 0 || page >= a.sh.pages);
-                if (lane == 0) {
-                    absent[buf][0] = (uint32_t)none;
-                    absent[buf][1] = (uint32_t)(none >> 32);
-                }
-            }
-            if (t0 + T::TOKENS < hi) words = load_words<D>(a, R, table, head, t0 + T::TOKENS, r.lo, hi);
+            store_words<D>(words, part, keys[buf], values[buf]);
+            absent[buf][part.sub] = page < 0 ? 1u : 0u;
+            page = page_next;
+            if (t0 + T::TOKENS < hi) words = load_words<D>(a, R, part, page, head, t0 + T::TOKENS, r.lo, hi);
+            page_next = page_of(t0 + 2 * T::TOKENS);
             __syncthreads();
             if (t0 >= w_end || t0 + T::TOKENS <= w_begin) continue;      // nothing that this wavefront's rows see
             f32x16 s[U];
@@ -186,7 +185,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
                     s[u] = mfma32(f.v, q[x].v, s[u]);
                 }
             }
-            const uint32_t none = absent[buf][0] | absent[buf][1];
+            uint32_t none = absent[buf][0] | absent[buf][1];
+            if (U > 1) none |= absent[buf][2] | absent[buf][3];
             if (t0 < all_begin || t0 + T::TOKENS > all_end || t0 + T::TOKENS > hi || __builtin_amdgcn_readfirstlane(none) != 0) {
                 int at = t0;
                 asm volatile("" : "+s"(at));       // (a branch: left alone, the comparisons are done for every tile)
@@ -196,7 +196,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const int k = 8 * (j >> 2) + 4 * hh + (j & 3), t = at + 32 * u + k;
-                        if (t >= stop || t < begin || ((absent[buf][u] >> k) & 1u)) s[u][j] = -__builtin_inff();
+                        if (t >= stop || t < begin || absent[buf][2 * u + (j >> 3)] != 0) s[u][j] = -__builtin_inff();
                     }
             }
             float top = s[0][0];
@@ -240,8 +240,8 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
         }
         if (32 * wave + i >= r.rows) continue;
         const float by = parts > 1 ? 1.0f : l > 0.f ? 1.0f / l : 0.f;
-        const int64_t part = parts > 1 ? kv4_part<true>(a, b, head, row, orow, h) + split : 0;
-        if (parts > 1 && hh == 0) a.many.part_ml[part] = float2{m, l};
+        const int64_t at = parts > 1 ? kv4_part<true>(a, b, head, row, orow, h) + split : 0;
+        if (parts > 1 && hh == 0) a.many.part_ml[at] = float2{m, l};
         // rows of the output tiles: register j of lane half hh is row 8 (j / 4) + 4 hh + j % 4; eight neighbouring dimensions lie in E
         // registers of every tile
 #pragma unroll
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
 #pragma unroll
             for (int e = 0; e < 8; ++e) v[e] = o[e / T::E][j + e % T::E] * by;
             if (parts > 1) {
-                f32x4* p = reinterpret_cast<f32x4*>(a.many.part_o + part * D + 8 * word);
+                f32x4* p = reinterpret_cast<f32x4*>(a.many.part_o + at * D + 8 * word);
                 p[0] = f32x4{v[0], v[1], v[2], v[3]};
                 p[1] = f32x4{v[4], v[5], v[6], v[7]};
             } else if (a.sh.out_type == LQER_F32) {
