@@ -49,12 +49,11 @@ struct Part {
     }
 };
 
-// page: of the wavefront's 16 tokens, -1 where they are not there.  [from, end): what the workgroup's rows see of the part.
+// page: of the wavefront's 16 tokens, one of the pool's.  (No branch here, and no use of what is loaded: the words are waited for when the
+// tile before them is done.)
 template <int D>
-__device__ __forceinline__ Words load_words(const Kv4Args& a, const Kv4Record<D> R, const Part<D>& part, int page, int head, int t0, int from, int end) {
-    Words w{};
-    if (page < 0) return w;
-    const int t = t0 + 16 * part.sub, off = t & ((1 << a.P_bits) - 1);
+__device__ __forceinline__ void load_words(const Kv4Args& a, const Kv4Record<D> R, const Part<D>& part, int page, int head, int t0, Words& w) {
+    const int off = (t0 + 16 * part.sub) & ((1 << a.P_bits) - 1);
     const uint8_t* const rec = a.pool + ((int64_t)page * a.sh.kv_heads + head) * R.bytes();
     if (part.k) {
         w.k = *reinterpret_cast<const u32x4*>(rec + R.key(off) + (uint32_t)(part.t * (D / 2) + 16 * part.c));
@@ -64,13 +63,14 @@ __device__ __forceinline__ Words load_words(const Kv4Args& a, const Kv4Record<D>
         w.v = *reinterpret_cast<const u32x4*>(rec + R.value(off / 4) + (uint32_t)(part.four * (2 * D) + part.word * 16));
         w.ve = *reinterpret_cast<const uint32_t*>(rec + R.value_exp(off / 4) + (uint32_t)(part.four * (D / 4) + part.word / 2 * 4));
     }
-    if (t < from || t + 16 > end) {
-        // tokens that no row sees may hold anything: their weights are 0, and meet a finite number
-        const int before = from - (t + 4 * part.four), n = end - (t + 4 * part.four);
-        if (before > 0) w.ve = before < 4 ? w.ve >> (8 * before) << (8 * before) : 0u;
-        if (n < 4) w.ve = n > 0 ? w.ve & ((1u << (8 * n)) - 1u) : 0u;
-    }
-    return w;
+}
+
+// The values' exponents of tokens outside [from, end) cleared: they may hold anything, their weights are 0 and meet a finite number.
+template <int D>
+__device__ __forceinline__ void clear_unseen(const Part<D>& part, int t0, int from, int end, Words& w) {
+    const int t = t0 + 16 * part.sub + 4 * part.four, before = from - t, n = end - t;
+    if (before > 0) w.ve = before < 4 ? w.ve >> (8 * before) << (8 * before) : 0u;
+    if (n < 4) w.ve = n > 0 ? w.ve & ((1u << (8 * n)) - 1u) : 0u;
 }
 
 // ... and into LDS as operands.  Keys: [32 tokens][step of 16 dimensions][64 lanes][16 B]; values: [tile of 32 output dimensions][step of 16
@@ -118,7 +118,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
     constexpr int QS = D / 16, NO = D / 32, U = T::TOKENS / 32;
     __shared__ __align__(16) uint8_t keys[2][T::KEYS];
     __shared__ __align__(16) uint8_t values[2][T::KEYS];
-    __shared__ uint32_t absent[2][4];              // whether a tile's 16 tokens have a page that is none of the pool's
+    __shared__ __align__(16) uint32_t absent[2][4];              // whether a tile's 16 tokens have a page that is none of the pool's
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 31, hh = lane >> 5;
     const int head = blockIdx.y % a.sh.kv_heads, b = blockIdx.z, split = blockIdx.x;
     Kv4Rows r = kv4_request(a, b);
@@ -157,36 +157,44 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
 #pragma unroll
             for (int j = 0; j < 16; ++j) o[x][j] = 0.f;
         float m = -__builtin_inff(), l = 0.f;
-        const auto page_of = [&](int t0) {         // -1: none of the pool's
+        int page_base = 0, page_of_lane = 0, page = 0;         // 64 entries of the request's table, one to a lane; the next words' page
+        bool fresh = true;
+        const auto fetch = [&](int t0, Words& w) {
             const int index = (t0 + 16 * part.sub) >> a.P_bits;
-            const int page = t0 < hi && index < a.sh.table_ld ? table[index] : -1;
-            return page < a.sh.pages ? page : -1;
+            if (fresh || index - page_base >= 64) {
+                page_base = index;
+                page_of_lane = index + lane < a.sh.table_ld ? table[index + lane] : -1;
+                fresh = false;
+            }
+            page = __builtin_amdgcn_readlane(page_of_lane, index - page_base);
+            if (page >= a.sh.pages) page = -1;
+            load_words<D>(a, R, part, page < 0 ? 0 : page, head, t0, w);
         };
-        int page = page_of(lo), page_next = page_of(lo + T::TOKENS);
-        Words words = load_words<D>(a, R, part, page, head, lo, r.lo, hi);
+        Words words;
+        if (lo < hi) fetch(lo, words);
         int buf = 0;
         for (int t0 = lo; t0 < hi; t0 += T::TOKENS, buf ^= 1) {
+            if (page < 0 || t0 < r.lo || t0 + T::TOKENS > hi) clear_unseen<D>(part, t0, page < 0 ? hi : r.lo, hi, words);
             store_words<D>(words, part, keys[buf], values[buf]);
             absent[buf][part.sub] = page < 0 ? 1u : 0u;
-            page = page_next;
-            if (t0 + T::TOKENS < hi) words = load_words<D>(a, R, part, page, head, t0 + T::TOKENS, r.lo, hi);
-            page_next = page_of(t0 + 2 * T::TOKENS);
+            if (t0 + T::TOKENS < hi) fetch(t0 + T::TOKENS, words);
             __syncthreads();
             if (t0 >= w_end || t0 + T::TOKENS <= w_begin) continue;      // nothing that this wavefront's rows see
+            const u32x4 gone = *reinterpret_cast<const u32x4*>(absent[buf]);
             f32x16 s[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int j = 0; j < 16; ++j) s[u][j] = 0.f;
 #pragma unroll
-                for (int x = 0; x < QS; ++x) {
+            for (int x = 0; x < QS; ++x)
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
                     Frag f;
                     f.u = *reinterpret_cast<const u32x4*>(keys[buf] + u * (32 * D * 2) + (x * 64 + lane) * 16);
                     s[u] = mfma32(f.v, q[x].v, s[u]);
                 }
-            }
-            uint32_t none = absent[buf][0] | absent[buf][1];
-            if (U > 1) none |= absent[buf][2] | absent[buf][3];
+            const uint32_t none = U > 1 ? gone[0] | gone[1] | gone[2] | gone[3] : gone[0] | gone[1];
             if (t0 < all_begin || t0 + T::TOKENS > all_end || t0 + T::TOKENS > hi || __builtin_amdgcn_readfirstlane(none) != 0) {
                 int at = t0;
                 asm volatile("" : "+s"(at));       // (a branch: left alone, the comparisons are done for every tile)
@@ -196,7 +204,7 @@ __global__ __launch_bounds__(256, D == 256 ? 1 : 2) void kv4_many_kernel(Kv4Args
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         const int k = 8 * (j >> 2) + 4 * hh + (j & 3), t = at + 32 * u + k;
-                        if (t >= stop || t < begin || absent[buf][2 * u + (j >> 3)] != 0) s[u][j] = -__builtin_inff();
+                        if (t >= stop || t < begin || gone[2 * u + (j >> 3)] != 0) s[u][j] = -__builtin_inff();
                     }
             }
             float top = s[0][0];
