@@ -463,9 +463,9 @@ def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, ele
         if h.shape != shape or not h.is_cuda or h.dtype != residual.dtype or (h.stride(1) != 1 and cols > 1):
             _refuse("h_out", "of residual's shape and type, on the GPU, its rows contiguous")
         r_ptr, h_ptr, ldr, ldh, res_type = residual.data_ptr(), h.data_ptr(), _stride(residual, rows, cols), _stride(h, rows, cols), h.dtype == bf16
-    codes = x.new_empty(shape, dtype=torch.int8)
+    codes = torch.empty_like(x, dtype=torch.int8, memory_format=torch.contiguous_format)
     exps = x.new_empty((rows, cols // 16), dtype=torch.uint8)
-    v = x.new_empty(shape, dtype=bf16) if values else None
+    v = torch.empty_like(codes, dtype=bf16) if values else None
     st = L.lqer_rmsnorm_mx(x.data_ptr(), x.dtype == bf16, rows, cols, _stride(x, rows, cols), r_ptr, ldr, h_ptr, ldh, res_type,
                            weight.data_ptr(), weight.dtype == bf16, eps, elem_bits, codes.data_ptr(), exps.data_ptr(),
                            v.data_ptr() if values else None, cols, _stream())

@@ -411,6 +411,10 @@ hipError_t launch_d(const Kv4Args& a, hipStream_t s) {
     return join<D, false>(a, s);
 }
 
+// Up to so many cached tokens a workgroup of the kernel for few rows takes all of them, ten steps a wavefront: about as long as parts of one step
+// and the launch that joins them, and one launch less for the host.
+constexpr int64_t kWholeTokens = 1280;
+
 // The cached tokens of `lots` tiles cut into parts: `least` tokens at least, and no more than give `wanted` workgroups, all at work at once.
 void cut(Kv4Plan& p, int64_t seen, int64_t lots, int64_t least, int64_t wanted) {
     int64_t chunk = (seen * lots / wanted + least - 1) / least * least;
@@ -453,7 +457,7 @@ size_t plan_kv4(Kv4Args& a, void* workspace) {
     const int64_t heads = (int64_t)sh.n_requests * sh.kv_heads;
     // 128 tokens are a step of 32 for each wavefront of a workgroup, 512 are eight steps of a workgroup for many rows: those keep two
     // workgroups to a compute unit, the others three
-    cut(a.few, seen, heads * a.few.row_tiles, 128, 768);
+    cut(a.few, seen, heads * a.few.row_tiles, seen <= kWholeTokens ? seen : 128, 768);
     cut(a.many, seen, heads * a.many.row_tiles, 512, 512);
     size_t at = 0;
     const auto place = [&](Kv4Plan& p, int64_t n) {
