@@ -1,0 +1,94 @@
+"""The decoder block of examples/decoder_block.py: its calls together, against the oracle's statement of the same block in 64 bits.
+
+Tolerance, derived.  Every call's own error is tested by itself; here what is rounded between them adds up: q as bf16 (2^-8 of each value), and
+codes of the norms and of the linears' inputs that fall on the other side of a tie because their input differs by such a rounding (one step
+of 2^-6 of the block's largest value, for a share of the values of about the rounding over the step).  A relative Frobenius error of 2^-8 in what a
+linear takes in is 2^-8 in what it gives, so that the block stays within a few times 2^-8: asserted is 2^-5."""
+import importlib.util
+import os
+
+import numpy as np
+import pytest
+
+from oracle import block as ob
+from oracle import mxint
+
+pytestmark = pytest.mark.gpu
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def example():
+    spec = importlib.util.spec_from_file_location("decoder_block", os.path.join(ROOT, "examples", "decoder_block.py"))
+    m = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(m)
+    return m
+
+
+def _linear(layer, x):
+    """X_q W_q + (X_q A_k) B_k of a layer's exported bytes, in 64 bits."""
+    from paper_2402_02446_amd import binding
+    d = binding.lqer_layer_export(layer)
+    W = mxint.mx_dequantize(mxint.unpack_int4(d["Wc"]), d["We"], 4)
+    A, B = mxint.mx_dequantize(d["Ac"], d["Ae"], 8), mxint.mx_dequantize(d["Bc"], d["Be"], 8)
+    xq = mxint.mx_dequantize(*mxint.mx_quantize(x, 8), 8)
+    return xq @ W.T + (xq @ A.T) @ B.T
+
+
+def _rotate(x, positions):
+    half = x.shape[-1] // 2
+    angle = positions[:, None] * 10000.0 ** (-np.arange(half) / half)
+    cos, sin = np.cos(angle)[:, None], np.sin(angle)[:, None]
+    return np.concatenate([x[..., :half] * cos - x[..., half:] * sin, x[..., half:] * cos + x[..., :half] * sin], -1)
+
+
+def _oracle_step(blk, x, residual, past, new, ids):
+    """The block in 64 bits; past[b]: the quantized keys and values of request b so far, extended here."""
+    f = lambda t: t.double().cpu().numpy()  # noqa: E731
+    h = x + residual
+    n1 = ob.rmsnorm(h, f(blk.norm1), float(np.float32(1e-5)))
+    q, k, v = _linear(blk.q, n1), _linear(blk.k, n1), _linear(blk.v, n1)
+    values = mxint.mx_dequantize(*mxint.mx_quantize(n1, 8), 8)
+    q, _ = ob.adapters(values, ids, f(blk.A), f(blk.B), q)
+    D, G = blk.head_dim, blk.q_heads // blk.kv_heads
+    q, k, v = (t.reshape(t.shape[0], -1, D) for t in (q, k, v))
+    out, first = np.zeros(q.shape), 0
+    for b, n in enumerate(new):
+        rows = slice(first, first + n)
+        first += n
+        start = past[b][0].shape[0]
+        pos = np.arange(start, start + n)
+        kq, vq = (ob.kv4_values(*ob.kv4_quantize(t)).reshape(t.shape) for t in (_rotate(k[rows], pos), v[rows]))
+        past[b] = (np.concatenate([past[b][0], kq]), np.concatenate([past[b][1], vq]))
+        qr = _rotate(q[rows], pos)
+        for head in range(blk.q_heads):
+            out[rows, head], _ = ob.attention(qr[:, head], past[b][0][:, head // G], past[b][1][:, head // G], blk.scale, np.zeros(n, int), pos + 1)
+    h = h + _linear(blk.o, out.reshape(out.shape[0], -1))
+    n2 = ob.rmsnorm(h, f(blk.norm2), float(np.float32(1e-5)))
+    gate, up = _linear(blk.gate, n2), _linear(blk.up, n2)
+    return _linear(blk.down, gate / (1 + np.exp(-gate)) * up), h
+
+
+def test_prompts_then_tokens(example):
+    import torch
+    blk = example.Block(hidden=256, mlp=512, q_heads=4, kv_heads=2, head_dim=64)
+    ids = np.array([2, -1, 0], np.int32)
+    cache = example.Cache(40, 2, 16, 64, 3, 128)
+    past = [(np.zeros((0, 2, 64)), np.zeros((0, 2, 64))) for _ in ids]
+    rng = np.random.default_rng(5)
+    for new in ([37, 70, 1], [1, 1, 1], [1, 3, 0], [1, 1, 1]):
+        T = sum(new)
+        x, r = (rng.standard_normal((T, 256)).astype(np.float32) for _ in range(2))
+        token_ids = np.repeat(ids, new)
+        y, res = blk.step(torch.from_numpy(x).cuda(), torch.from_numpy(r).cuda(), cache, cache.take(new), torch.from_numpy(token_ids).cuda())
+        ry, rres = _oracle_step(blk, x.astype(np.float64), r.astype(np.float64), past, new, token_ids)
+        for got, want in ((y, ry), (res, rres)):
+            got = got.double().cpu().numpy()
+            assert np.all(np.isfinite(got))
+            assert np.linalg.norm(got - want) <= 2.0 ** -5 * np.linalg.norm(want)
+    assert cache.lengths.tolist() == [40, 75, 3]
+
+
+def test_the_example_runs(example, capsys):
+    example.main()
+    assert "decode steps of 3 requests" in capsys.readouterr().out
