@@ -399,7 +399,8 @@ int lqer_adapters_forward(const uint16_t* X_dev, int64_t M, int64_t K, int64_t l
  * eight consecutive dimensions of one token as signs and magnitudes: byte i = |e_i| in bits 0-2, the sign of e_(4 + (i + 3) % 4)
  * in bit 3, |e_(4+i)| in bits 4-6, the sign of e_i in bit 7; a zero has no sign.  The values of four tokens lie side by side because
  * the product with the weights contracts over tokens: one 16-byte load holds four terms of eight output dimensions.
- * Pages need no clearing: what no length covers is never used.  lqer_kv4_page_bytes returns 0 for sizes the format does not have.
+ * Pages need no clearing: what no length covers is never used.  A pool, and a request's table, hold at most 2^30 tokens (LQER_ERR_SHAPE).
+ * lqer_kv4_page_bytes returns 0 for sizes the format does not have.
  *
  * lqer_kv4_append quantizes the step's keys and values into the pool:
  *   k_dev, v_dev  [T][kv_heads][head_dim] with token strides ldk, ldv (elements, >= kv_heads * head_dim, multiples of
@@ -427,7 +428,8 @@ int lqer_kv4_append(uint8_t* pool_dev, int64_t pages, int page_tokens, int kv_he
  *   out_dev     out_type [Tq][q_heads][head_dim], token stride ldo (multiple of 8); rows that no request covers are left alone
  *   workspace_dev  lqer_kv4_attention_workspace_bytes(...) of the same numbers, 256-byte aligned, scratch
  * q_heads is a multiple of kv_heads.  Scores, running maxima, sums and outputs are fp32; the weights exp(s - max) enter the product
- * with V as two bf16 terms (relative 2^-16).
+ * with V as two bf16 terms (relative 2^-16) where a request has up to 64 rows (queries times query heads of a cached head), as one (2^-8 at
+ * most) where it has more: prompts are bound by the matrix instructions.
  */
 typedef struct {
     int n_requests;

@@ -21,13 +21,14 @@ bool adapter_sizes(AdapterArgs& a, int64_t M, int64_t K, int64_t N, int R, int n
 }
 
 bool kv4_format_ok(int P, int D) { return P >= 16 && P <= 1024 && (P & (P - 1)) == 0 && (D == 64 || D == 128 || D == 256); }
-// (slots and token counts are 32 bits wide on the device)
-bool kv4_pool_ok(int64_t pages, int P, int heads) { return pages > 0 && heads > 0 && heads <= 1024 && pages <= kMaxGrid / P; }
+// (slots, and sums of two token counts, are 32 bits wide on the device)
+constexpr int64_t kMaxTokens = 1 << 30;
+bool kv4_pool_ok(int64_t pages, int P, int heads) { return pages > 0 && heads > 0 && heads <= 1024 && pages <= kMaxTokens / P; }
 
 int kv4_shape_status(const lqer_kv4_shape& s) {
     if (!kv4_format_ok(s.page_tokens, s.head_dim) || !type_ok(s.out_type)) return LQER_ERR_UNSUPPORTED;
     if (!kv4_pool_ok(s.pages, s.page_tokens, s.kv_heads) || s.q_heads <= 0 || s.q_heads > 65536 || s.q_heads % s.kv_heads != 0) return LQER_ERR_SHAPE;
-    if (s.n_requests < 0 || s.n_requests > 65535 || s.table_ld <= 0 || s.table_ld > kMaxGrid / s.page_tokens || s.Tq < 0 || s.Tq > kMaxGrid / 2 / s.q_heads)
+    if (s.n_requests < 0 || s.n_requests > 65535 || s.table_ld <= 0 || s.table_ld > kMaxTokens / s.page_tokens || s.Tq < 0 || s.Tq > kMaxGrid / 2 / s.q_heads)
         return LQER_ERR_SHAPE;
     const int64_t row = (int64_t)s.q_heads * s.head_dim;
     if (!stride_ok(s.ldq, row, LQER_BF16) || !stride_ok(s.ldo, row, LQER_BF16)) return LQER_ERR_SHAPE;

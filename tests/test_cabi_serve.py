@@ -74,7 +74,7 @@ def _append(L, **kw):
 
 @pytest.mark.parametrize("status, bad", [
     (0, dict(T=0)), (NULL, dict(pool=None)), (NULL, dict(k=None)), (NULL, dict(v=None)), (NULL, dict(slots=None)), (UNSUPPORTED, dict(P=17)),
-    (UNSUPPORTED, dict(D=80)), (UNSUPPORTED, dict(t=2)), (SHAPE, dict(T=-1)), (SHAPE, dict(pages=0)), (SHAPE, dict(pages=1 << 27)),
+    (UNSUPPORTED, dict(D=80)), (UNSUPPORTED, dict(t=2)), (SHAPE, dict(T=-1)), (SHAPE, dict(pages=0)), (SHAPE, dict(pages=(1 << 26) + 1)),
     (SHAPE, dict(heads=0)), (SHAPE, dict(heads=1025)), (SHAPE, dict(ldk=120)), (SHAPE, dict(ldv=132)), (SHAPE, dict(k=P + 2)), (SHAPE, dict(v=P + 4)),
     (SHAPE, dict(pool=P + 8)), (SHAPE, dict(slots=P + 2))])
 def test_kv4_append(L, status, bad):
@@ -93,7 +93,7 @@ def _attend(L, ptrs=None, ws=P, ws_bytes=1 << 30, **kw):
 @pytest.mark.parametrize("status, bad", [
     (0, dict(Tq=0)), (0, dict(n_requests=0)), (UNSUPPORTED, dict(head_dim=96)), (UNSUPPORTED, dict(page_tokens=2048)), (UNSUPPORTED, dict(out_type=3)),
     (SHAPE, dict(q_heads=7)), (SHAPE, dict(q_heads=0)), (SHAPE, dict(kv_heads=0)), (SHAPE, dict(n_requests=-1)), (SHAPE, dict(n_requests=65536)),
-    (SHAPE, dict(table_ld=0)), (SHAPE, dict(table_ld=1 << 28)), (SHAPE, dict(Tq=-1)), (SHAPE, dict(Tq=1 << 31)), (SHAPE, dict(pages=0)),
+    (SHAPE, dict(table_ld=0)), (SHAPE, dict(table_ld=(1 << 26) + 1)), (SHAPE, dict(Tq=-1)), (SHAPE, dict(Tq=1 << 31)), (SHAPE, dict(pages=0)),
     (SHAPE, dict(ldq=511)), (SHAPE, dict(ldq=516)), (SHAPE, dict(ldo=504)), (SHAPE, dict(max_q=-1)), (SHAPE, dict(max_kv=-1)), (SHAPE, dict(causal=2)),
     (SHAPE, dict(window=-1)), (SHAPE, dict(scale=float("nan"))), (NULL, dict(ptrs=dict(pool=None))), (NULL, dict(ptrs=dict(q=None))),
     (NULL, dict(ptrs=dict(cu=None))), (NULL, dict(ptrs=dict(kv=None))), (NULL, dict(ptrs=dict(table=None))), (NULL, dict(ptrs=dict(out=None))),
