@@ -82,7 +82,7 @@ def test_kv4_append(L, status, bad):
 
 
 def _attend(L, ptrs=None, ws=P, ws_bytes=1 << 30, **kw):
-    a = dict(n_requests=2, q_heads=8, kv_heads=2, head_dim=64, page_tokens=16, table_ld=40, pages=100, Tq=2, ldq=512, ldo=512, max_q=1, max_kv=600,
+    a = dict(n_requests=2, q_heads=8, kv_heads=2, head_dim=64, page_tokens=16, table_ld=400, pages=900, Tq=2, ldq=512, ldo=512, max_q=1, max_kv=6000,
              causal=1, window=0, scale=0.125, out_type=1)
     a.update(kw)
     p = dict(pool=P, q=P, cu=P, kv=P, table=P, out=P)
@@ -101,6 +101,19 @@ def _attend(L, ptrs=None, ws=P, ws_bytes=1 << 30, **kw):
     (WORKSPACE, dict(ws=None)), (WORKSPACE, dict(ws=P + 16)), (WORKSPACE, dict(ws_bytes=16))])
 def test_kv4_attention(L, status, bad):
     assert _attend(L, **bad) == status
+
+
+def test_kv4_attention_workspace(L):
+    """Parts of a long axis, and of few tiles of many rows, are joined in the workspace; short caches need none."""
+    def need(**kw):
+        a = dict(n_requests=2, q_heads=8, kv_heads=2, head_dim=64, page_tokens=16, table_ld=400, pages=900, Tq=2, ldq=512, ldo=512, max_q=1,
+                 max_kv=6000, causal=1, window=0, scale=0.125, out_type=1)
+        a.update(kw)
+        return L.lqer_kv4_attention_workspace_bytes(binding.C.byref(binding.Kv4Shape(*a.values())))
+    assert need() > 0 and need(max_kv=600) == 0 and need(window=500) == 0 and need(q_heads=7) == 0 and need(Tq=0) == 0
+    assert need(Tq=200, max_q=100) > 0
+    assert need(n_requests=400, Tq=400 * 2000, max_q=2000, max_kv=100000) == 0          # enough tiles without parts
+    assert need() % 256 == 0 and need(Tq=1001, n_requests=2, max_q=1000) < 600 << 20
 
 
 def test_kv4_attention_without_a_shape(L):
