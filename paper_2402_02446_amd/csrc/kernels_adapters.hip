@@ -5,9 +5,9 @@
 // bounds them: with few tokens the bytes of the A and B of the adapters in the batch, each read by one group; with many the
 // bytes of X and of Y in and out.
 //
-// Groups.  Up to 64 tokens every wavefront finds its group by itself: one comparison of all ids with its own (a ballot) gives the
-// tokens of the adapter, and the first of them keeps the workgroup, the others' end.  Beyond, one workgroup sorts the tokens by
-// adapter first and lists tiles of up to 64 of them.  Tokens without an adapter are a group of rank 0: their rows are copied.
+// Groups.  Up to 64 tokens a wavefront of every workgroup finds the groups that there are by itself: of the tokens with one adapter one finds its own
+// number in a table in LDS; the workgroups are shared out among the groups.  Beyond, one workgroup sorts the tokens by adapter first
+// and lists tiles of up to 16 or 64 of them.  Tokens without an adapter are a group of rank 0: their rows are copied.
 //
 // Matrix instructions: 16 x 16 x 32 bf16.  Projection: ranks as rows and tokens as columns, so that a lane holds four neighbouring ranks
 // of one token.  Second product: tokens as rows and as columns every NT-th output column, so that a lane holds NT neighbouring columns
@@ -21,7 +21,8 @@ namespace lqer {
 
 namespace {
 
-constexpr int kTile = 64;              // most tokens of a group's tile
+constexpr int64_t kNarrowTokens = 1024;  // most tokens that are sorted into tiles of 16
+constexpr int kWide = 64;              // most tokens of a tile; and the calls whose tokens need no sorting
 
 struct Group {
     int adapter;                       // -1: none
@@ -35,11 +36,11 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t m) {
 }
 
 // What this workgroup works on, and its group's tokens in rows[] (LDS).  Uniform over the workgroup; holds barriers.
-// FEW: all workgroups are shared out evenly among the groups that there are; otherwise `parts` to each tile.
-template <bool FEW>
+// Without sorting, parts = 0: all workgroups are shared out evenly among the groups that there are; otherwise `parts` to each group or tile.
+template <bool SORTED>
 __device__ __forceinline__ Group find_group(const AdapterArgs& a, int parts, int* rows) {
     __shared__ Group found;
-    if (FEW) {
+    if (!SORTED) {
         __shared__ uint8_t seen[kMaxAdapters + 1];
         if (threadIdx.x < 64) {
             const int lane = threadIdx.x;
@@ -71,28 +72,28 @@ __device__ __forceinline__ int rank_of(const AdapterArgs& a, int adapter) {
     return a.ranks ? min(max(a.ranks[adapter], 0), a.R) : a.R;
 }
 
-// T[split][token][rank]: RT tiles of 16 ranks.  FEW: the four wavefronts share a group's chunks of K; otherwise each has 16 of the
-// tile's tokens.
-template <int RT, bool FEW>
+// T[split][token][rank]: RT tiles of 16 ranks.  WIDE: each of the four wavefronts has 16 of the tile's 64 tokens; otherwise they share
+// the chunks of K, 16 tokens at a time.
+template <int RT, bool SORTED, bool WIDE>
 __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
-    __shared__ int rows[kTile];
-    __shared__ f32x4 part[FEW ? 4 * RT * 64 : 1];
-    const Group gr = find_group<FEW>(a, a.splits, rows);
+    __shared__ int rows[kWide];
+    __shared__ f32x4 part[WIDE ? 1 : 4 * RT * 64];
+    const Group gr = find_group<SORTED>(a, a.splits, rows);
     const int rank = rank_of(a, gr.adapter);
     if (gr.part >= gr.parts || rank == 0) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, g = lane >> 4;
     const int64_t per = a.k_split, k_lo = gr.part * per, k_hi = min(a.K, k_lo + per);
     const uint16_t* const A = a.A + (int64_t)gr.adapter * a.R * a.K;
     float* const T = a.T + (int64_t)gr.part * a.M * a.Rp;
-    for (int t0 = FEW ? 0 : 16 * wave; t0 < gr.count; t0 += FEW ? 16 : kTile) {
+    for (int t0 = WIDE ? 16 * wave : 0; t0 < gr.count; t0 += WIDE ? kWide : 16) {
         const int64_t row = rows[min(t0 + i, gr.count - 1)];
         const uint16_t* const x = a.X + row * a.ldx;
         f32x4 acc[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
         // AHEAD chunks' loads are issued before the first one's products
-        constexpr int AHEAD = RT <= 2 ? 4 : RT == 4 ? 2 : 1, STEP = FEW ? 256 : 64;
-        for (int64_t k0 = k_lo + (FEW ? 64 * wave : 0); k0 < k_hi; k0 += AHEAD * STEP) {
+        constexpr int AHEAD = RT <= 2 ? 4 : RT == 4 ? 2 : 1, STEP = WIDE ? 64 : 256;
+        for (int64_t k0 = k_lo + (WIDE ? 0 : 64 * wave); k0 < k_hi; k0 += AHEAD * STEP) {
             Frag xf[AHEAD][2], af[AHEAD][2][RT];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
@@ -115,7 +116,7 @@ __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
 #pragma unroll
                     for (int r = 0; r < RT; ++r) acc[r] = mfma16(af[u][h][r].v, xf[u][h].v, acc[r]);
         }
-        if (FEW) {                     // the wavefronts' sums, in order
+        if (!WIDE) {                   // the wavefronts' sums, in order
 #pragma unroll
             for (int r = 0; r < RT; ++r) part[(wave * RT + r) * 64 + lane] = acc[r];
             __syncthreads();
@@ -200,13 +201,13 @@ struct FourRows {
     }
 };
 
-template <int KK, int NT, bool FEW>
+template <int KK, int NT, bool SORTED, bool WIDE>
 __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
-    constexpr int TROWS = FEW ? 16 : kTile;
+    constexpr int TROWS = WIDE ? kWide : 16;
     constexpr int LD = 32 * KK + 8;                        // (a row's length in LDS: 16 bytes more than its ranks, off the same banks)
-    __shared__ int rows[kTile];
+    __shared__ int rows[kWide];
     __shared__ __align__(16) uint16_t terms[3][TROWS][LD];
-    const Group gr = find_group<FEW>(a, FEW ? 0 : a.parts, rows);
+    const Group gr = find_group<SORTED>(a, SORTED ? a.parts : 0, rows);
     const int blocks = (int)((a.N + 64 * NT - 1) / (64 * NT));
     const int columns = gr.parts > 0 ? (blocks + gr.parts - 1) / gr.parts : 0;
     if (gr.part >= gr.parts || (int64_t)gr.part * columns >= blocks) return;
@@ -338,7 +339,7 @@ __global__ __launch_bounds__(1024) void adapter_sort_kernel(AdapterArgs a) {
     int tokens = 0, tiles = 0;
     for (int b = b0; b < b1; ++b) {
         tokens += count[b];
-        tiles += (count[b] + kTile - 1) / kTile;
+        tiles += (count[b] + a.tile - 1) / a.tile;
     }
     int before_tokens = tokens, before_tiles = tiles;      // sums over the threads before this one
 #pragma unroll
@@ -359,8 +360,8 @@ __global__ __launch_bounds__(1024) void adapter_sort_kernel(AdapterArgs a) {
     for (int b = b0; b < b1; ++b) {
         const int c = count[b];
         count[b] = before_tokens;
-        for (int s = 0; s < c; s += kTile)
-            a.tiles[before_tiles++] = AdapterTile{b < a.n ? b : -1, before_tokens + s, min(c - s, kTile), 0};
+        for (int s = 0; s < c; s += a.tile)
+            a.tiles[before_tiles++] = AdapterTile{b < a.n ? b : -1, before_tokens + s, min(c - s, a.tile), 0};
         before_tokens += c;
     }
     __syncthreads();
@@ -384,23 +385,25 @@ __global__ __launch_bounds__(1024) void adapter_sort_kernel(AdapterArgs a) {
     }
 }
 
-int64_t most_groups(int64_t M, int n) { return M <= kTile ? M : M / kTile + (M < n + 1 ? M : n + 1); }
+// the most groups (few tokens) or tiles that there can be
+int64_t most_groups(const AdapterArgs& a) { return a.tile == 0 ? a.M : a.M / a.tile + (a.M < a.n + 1 ? a.M : a.n + 1); }
 
 template <int RT>
-hipError_t project(const AdapterArgs& a, bool few, hipStream_t s) {
-    const dim3 grid((unsigned)(most_groups(a.M, a.n) * a.splits));
-    if (few) hipLaunchKernelGGL((adapter_project_kernel<RT, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((adapter_project_kernel<RT, false>), grid, dim3(256), 0, s, a);
+hipError_t project(const AdapterArgs& a, hipStream_t s) {
+    const dim3 grid((unsigned)(most_groups(a) * a.splits));
+    if (a.tile == 0) hipLaunchKernelGGL((adapter_project_kernel<RT, false, false>), grid, dim3(256), 0, s, a);
+    else if (a.tile < kWide) hipLaunchKernelGGL((adapter_project_kernel<RT, true, false>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((adapter_project_kernel<RT, true, true>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
 // A workgroup takes several blocks of columns one after another, T summed up once for all, where about eight workgroups
 // to a compute unit are left (few tokens: four, which share the groups that there are out evenly).
-template <int KK, int NT, bool FEW>
+template <int KK, int NT, bool SORTED, bool WIDE>
 hipError_t expand(AdapterArgs a, hipStream_t s) {
-    const int64_t blocks = (a.N + 64 * NT - 1) / (64 * NT), groups = most_groups(a.M, a.n);
+    const int64_t blocks = (a.N + 64 * NT - 1) / (64 * NT), groups = most_groups(a);
     int64_t grid = groups * blocks;
-    if (FEW) {
+    if (!SORTED) {
         if (grid > 1024) grid = 1024;              // (more than groups: M <= 64)
     } else {
         int64_t columns = grid / 2048;
@@ -408,27 +411,32 @@ hipError_t expand(AdapterArgs a, hipStream_t s) {
         a.parts = (int)((blocks + columns - 1) / columns);
         grid = groups * a.parts;
     }
-    hipLaunchKernelGGL((adapter_expand_kernel<KK, NT, FEW>), dim3((unsigned)grid), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((adapter_expand_kernel<KK, NT, SORTED, WIDE>), dim3((unsigned)grid), dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
 template <int KK>
-hipError_t expand(const AdapterArgs& a, bool few, hipStream_t s) {
-    if (!few) return expand<KK, KK == 4 ? 2 : 4, false>(a, s);     // (ranks above 64: fewer columns, or their B leaves one wavefront a SIMD)
-    return a.M * ((a.N + 127) / 128) >= 1024 ? expand<KK, 2, true>(a, s) : expand<KK, 1, true>(a, s);
+hipError_t expand(const AdapterArgs& a, hipStream_t s) {
+    // (ranks above 64: fewer columns, or their B leaves one wavefront a SIMD)
+    if (a.tile == kWide) return expand<KK, KK == 4 ? 2 : 4, true, true>(a, s);
+    if (a.tile > 0) return expand<KK, KK == 4 ? 2 : 4, true, false>(a, s);
+    return a.M * ((a.N + 127) / 128) >= 1024 ? expand<KK, 2, false, false>(a, s) : expand<KK, 1, false, false>(a, s);
 }
 
 }  // namespace
 
 size_t plan_adapters(AdapterArgs& a, void* workspace) {
     a.Rp = (a.R + 15) / 16 * 16;
-    const bool few = a.M <= kTile;
+    // Up to 64 tokens need no sorting.  Tiles of 16 tokens, whose four wavefronts share K, as long as they are not many; of 64, which read A and B a quarter
+    // as often, beyond (us, 16 / 64: 251 tokens of 672 x 532 rank 128 16 / 20, 630 of 5696 x 2208 rank 64 23 / 39, 1000 of 4096 x 4096 rank 16 21 / 24;
+    // 1000 of 4096 x 11008 rank 64 with 24 adapters 48 / 44, 1500 of 4096 x 4096 rank 32 27 / 28, 3000 of 2048 x 2048 rank 128 56 / 55).
+    a.tile = a.M <= kWide ? 0 : a.M <= kNarrowTokens ? 16 : kWide;
     // Parts of K: at least 512 values each, at most 8 parts (that many loads sum T up at once), and with many tokens no more than give two
     // workgroups to a compute unit
     int64_t parts = (a.K + 511) / 512;
     if (parts > 8) parts = 8;
-    if (!few) {
-        const int64_t tiles = (a.M + kTile - 1) / kTile, want = (512 + tiles - 1) / tiles;
+    if (a.tile > 0) {
+        const int64_t tiles = (a.M + a.tile - 1) / a.tile, want = (512 + tiles - 1) / tiles;
         if (parts > want) parts = want;
     }
     a.k_split = ((a.K + parts - 1) / parts + 63) / 64 * 64;
@@ -440,11 +448,11 @@ size_t plan_adapters(AdapterArgs& a, void* workspace) {
     a.list = nullptr;
     a.tiles = nullptr;
     a.order = nullptr;
-    if (!few) {
+    if (a.tile > 0) {
         a.list = (int*)(base + at);
         at += 256;
         a.tiles = (AdapterTile*)(base + at);
-        at += up(most_groups(a.M, a.n) * (int64_t)sizeof(AdapterTile));
+        at += up(most_groups(a) * (int64_t)sizeof(AdapterTile));
         a.order = (int*)(base + at);
         at += up(a.M * 4);
     }
@@ -452,20 +460,19 @@ size_t plan_adapters(AdapterArgs& a, void* workspace) {
 }
 
 hipError_t launch_adapters(const AdapterArgs& a, hipStream_t s) {
-    const bool few = a.M <= kTile;
-    if (!few) {
+    if (a.tile > 0) {
         hipLaunchKernelGGL(adapter_sort_kernel, dim3(1), dim3(1024), (size_t)(a.n + 1) * 4, s, a);
         if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
     }
     hipError_t e;
-    if (a.R <= 16) e = project<1>(a, few, s);
-    else if (a.R <= 32) e = project<2>(a, few, s);
-    else if (a.R <= 64) e = project<4>(a, few, s);
-    else e = project<8>(a, few, s);
+    if (a.R <= 16) e = project<1>(a, s);
+    else if (a.R <= 32) e = project<2>(a, s);
+    else if (a.R <= 64) e = project<4>(a, s);
+    else e = project<8>(a, s);
     if (e != hipSuccess) return e;
-    if (a.R <= 32) return expand<1>(a, few, s);
-    if (a.R <= 64) return expand<2>(a, few, s);
-    return expand<4>(a, few, s);
+    if (a.R <= 32) return expand<1>(a, s);
+    if (a.R <= 64) return expand<2>(a, s);
+    return expand<4>(a, s);
 }
 
 }  // namespace lqer

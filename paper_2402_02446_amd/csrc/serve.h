@@ -40,6 +40,7 @@ struct AdapterArgs {
     int64_t N, ldyo;
     // set by plan_adapters
     int Rp;                // R in whole tiles of 16: T's row length
+    int tile;              // tokens of a tile; 0: few tokens, unsorted
     int splits;            // parts of K, of k_split values each
     int64_t k_split;
     float* T;              // [splits][M][Rp]
