@@ -147,7 +147,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
     __shared__ float join_m[WAVES][16], join_l[WAVES][16];
     // (the wavefront's number as a scalar: its steps, pages and their addresses are then computed once, not by every lane)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
-    const int head = blockIdx.y % a.sh.kv_heads, b = blockIdx.z, split = blockIdx.x;
+    const int head = blockIdx.x % a.sh.kv_heads, b = blockIdx.y, split = blockIdx.z;
     Kv4Rows r = kv4_request(a, b);
     if (!kv4_mine<false>(a, r)) return;
     const Kv4Record<D> R{a.P_bits};
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
     // (0 as the smallest normal number: a masked score is minus infinity)
     const float to_log2 = __builtin_fmaxf(__builtin_fabsf(a.sh.scale) * kLog2e, 0x1p-126f);
     const uint32_t turn = a.sh.scale < 0.f ? 0x80008000u : 0u;
-    for (int row0 = blockIdx.y / a.sh.kv_heads * 16; row0 < r.n * a.group; row0 += a.few.row_tiles * 16) {
+    for (int row0 = blockIdx.x / a.sh.kv_heads * 16; row0 < r.n * a.group; row0 += a.few.row_tiles * 16) {
         kv4_tile(a, r, row0, 16);
         int chunk;
         const int parts = kv4_parts<false>(a, r, chunk);
@@ -405,8 +405,9 @@ hipError_t launch_d(const Kv4Args& a, hipStream_t s) {
         if (e != hipSuccess) return e;
     }
     if (!a.few.run) return hipSuccess;
-    const unsigned y = (unsigned)(a.few.row_tiles * a.sh.kv_heads);
-    hipLaunchKernelGGL((kv4_few_kernel<D>), dim3((unsigned)a.few.splits, y, (unsigned)a.sh.n_requests), dim3(256), 0, s, a);
+    // (parts outermost: those that only the longest requests have come last, and what is at work is spread evenly)
+    const dim3 grid((unsigned)(a.few.row_tiles * a.sh.kv_heads), (unsigned)a.sh.n_requests, (unsigned)a.few.splits);
+    hipLaunchKernelGGL((kv4_few_kernel<D>), grid, dim3(256), 0, s, a);
     if (hipError_t e = hipGetLastError(); e != hipSuccess || a.few.splits == 1) return e;
     return join<D, false>(a, s);
 }
@@ -417,11 +418,10 @@ constexpr int64_t kWholeTokens = 1280;
 
 // The cached tokens of `lots` tiles cut into parts: `least` tokens at least, and no more than give `wanted` workgroups, all at work at once.
 void cut(Kv4Plan& p, int64_t seen, int64_t lots, int64_t least, int64_t wanted) {
-    int64_t chunk = (seen * lots / wanted + least - 1) / least * least;
-    if (chunk < least) chunk = least;
+    int64_t chunk = std::max(least, (seen * lots / wanted + 127) / 128 * 128);
     if (chunk > (1 << 30)) chunk = 1 << 30;
     p.chunk = (int)chunk;
-    p.splits = (int)((seen + chunk - 1) / chunk);
+    p.splits = (int)std::min<int64_t>((seen + chunk - 1) / chunk, 65535);
 }
 
 }  // namespace
@@ -455,9 +455,13 @@ size_t plan_kv4(Kv4Args& a, void* workspace) {
     int64_t seen = std::max(sh.max_kv, 1);
     if (sh.window > 0) seen = std::min<int64_t>(seen, (int64_t)sh.window + sh.max_q + 31);
     const int64_t heads = (int64_t)sh.n_requests * sh.kv_heads;
-    // 128 tokens are a step of 32 for each wavefront of a workgroup, 512 are eight steps of a workgroup for many rows: those keep two
-    // workgroups to a compute unit, the others three
-    cut(a.few, seen, heads * a.few.row_tiles, seen <= kWholeTokens ? seen : 128, 768);
+    // 128 tokens are a step of 32 for each wavefront of a workgroup, 512 are eight tiles of a workgroup for many rows: those keep two
+    // workgroups to a compute unit, the others three: 768.  Short parts of few rows (up to nine steps a wavefront) are cut a little finer: where the
+    // requests' lengths differ many of the 768 have nothing to do (us, 1024 / 768: 16 requests of up to 4096 tokens 24 / 28, all of 4096 30 / 30, 8 of up to
+    // 12538 32 / 36; long ones not: 4 of 100003 110 / 103), but not below two steps, which the joining would outweigh (one of 16000 17 / 14).
+    const int64_t lots = heads * a.few.row_tiles;
+    if (seen <= kWholeTokens) cut(a.few, seen, lots, seen, 768);
+    else if (cut(a.few, seen, lots, 128, 768); a.few.chunk <= 1152) cut(a.few, seen, lots, 256, 1024);
     cut(a.many, seen, heads * a.many.row_tiles, 512, 512);
     size_t at = 0;
     const auto place = [&](Kv4Plan& p, int64_t n) {
