@@ -96,13 +96,28 @@ __device__ __forceinline__ void store_words(const Words& w, const Part<D>& part,
 #pragma unroll
             for (int x = 0; x < 4; ++x) t[j][x] = f.u[x];
         }
-        // tokens 4 hh .. and 8 + 4 hh .. of the 16: the two halves of lane half hh
-        uint8_t* const at = values + (part.sub * 64 + (part.four & 1) * 32 + T::E * part.word) * 16 + (part.four >> 1) * 8;
+        u32x2 half[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const uint32_t sel = e & 1 ? 0x07060302u : 0x05040100u;
-            const u32x2 half = {__builtin_amdgcn_perm(t[1][e / 2], t[0][e / 2], sel), __builtin_amdgcn_perm(t[3][e / 2], t[2][e / 2], sel)};
-            *reinterpret_cast<u32x2*>(at + ((e / T::E) * (T::TOKENS / 16) * 64 + e % T::E) * 16) = half;
+            half[e] = u32x2{__builtin_amdgcn_perm(t[1][e / 2], t[0][e / 2], sel), __builtin_amdgcn_perm(t[3][e / 2], t[2][e / 2], sel)};
+        }
+        // tokens 4 hh .. and 8 + 4 hh .. of the 16: the two halves of lane half hh
+        constexpr int BLOCK = T::TOKENS / 16 * 64;                 // cells of a tile of output dimensions
+        uint8_t* const at = values + (part.sub * 64 + (part.four & 1) * 32 + T::E * part.word) * 16;
+        if (D == 64) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) *reinterpret_cast<u32x2*>(at + ((e / T::E) * BLOCK + e % T::E) * 16 + (part.four >> 1) * 8) = half[e];
+        } else {
+            // the other half of a cell is 32 lanes away: the lower lanes take both of the dimensions 0 to 3, the upper ones of 4 to 7, and write
+            // whole cells of 16 bytes (halves of 8 would meet in the same banks four at a time)
+            uint8_t* const mine = at + (part.four >> 1) * (4 / T::E) * BLOCK * 16;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const auto x = __builtin_amdgcn_permlane32_swap(half[e][0], half[e + 4][0], false, false);
+                const auto y = __builtin_amdgcn_permlane32_swap(half[e][1], half[e + 4][1], false, false);
+                *reinterpret_cast<u32x4*>(mine + ((e / T::E) * BLOCK + e % T::E) * 16) = u32x4{x[0], y[0], x[1], y[1]};
+            }
         }
     }
 }
