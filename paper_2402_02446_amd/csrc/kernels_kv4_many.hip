@@ -10,6 +10,11 @@
 // The running maximum is moved only when a score passes it by more than 2^8: until then the weights, relative to the older
 // maximum, are at most 2^8, which costs no precision, and the accumulators need no rescaling.  The weights enter the product as bf16
 // (relative 2^-8 at most), their sum in fp32.
+//
+// Measured: 2 x 2048 queries on up to 6144 tokens, 64 / 8 heads of 128 (374 GFLOP) 400 to 460 us from card to card; the matrix instructions are busy
+// 38 % of the cycles, vector instructions 50 %, LDS 34 %: with two wavefronts to a SIMD they come one after another.  Not faster: reads
+// of LDS scheduled ahead, exponentials pinned among the matrix instructions, wavefront priorities, tiles of 32 tokens with three workgroups
+// to a compute unit (13 % slower), 64 rows to a wavefront (35 % slower: 508 registers, one wavefront to a SIMD).
 #include "kv4_device.h"
 
 namespace lqer {

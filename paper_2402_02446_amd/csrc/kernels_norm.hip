@@ -9,6 +9,9 @@
 // The mean and v are computed in 64 bits, which run at fp32's rate here and hide behind the memory: what decides a code is
 // then h alone, not the order in which a row was summed.  v * 2^(fraction bits - e) is rounded to an integer by the addition of 1.5 * 2^52
 // in the same fused multiply-add: the low word of the sum is the code.
+//
+// Measured: 8192 rows of 8192 (fp32 x, bf16 residual, values) 128 to 132 us, 5.7 TB/s of what has to move (a large copy: 5.05); 203 of 4112 5.2 us;
+// one of 4096 3.4 us.
 #include "serve.h"
 #include "mx_device.h"
 
