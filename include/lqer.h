@@ -356,7 +356,7 @@ typedef enum { LQER_F32 = 0, LQER_BF16 = 1 } lqer_type;
  *                 consumers that take no codes, as lqer_adapters_forward
  * All pointers 16-byte aligned (exps_dev: any), strides multiples of 16 bytes; LQER_ERR_SHAPE otherwise.  h is the fp32 sum,
  * rounded once more where res_type is bf16 (v is computed from the fp32 sum); the mean and v are computed in 64
- * bits, so that a code is that of the exact v but for the rounding of h.  Inputs must be finite, eps >= 0 (a row of zeros with eps = 0 has
+ * bits, so that a code is that of the exact v but for the rounding of h.  Inputs must be finite, eps finite and >= 0 (a row of zeros with eps = 0 has
  * codes 0).  rows == 0 or cols == 0 is a no-op.
  */
 int lqer_rmsnorm_mx(const void* x_dev, int x_type, int64_t rows, int64_t cols, int64_t ldx,

@@ -486,23 +486,23 @@ def lqer_adapters_forward(X, ids, A, B, Y, out=None, ranks=None, scales=None, wo
     L, bf16, f32, i32 = _lib or lib(), torch.bfloat16, torch.float32, torch.int32
     n, R, K = A.shape
     M, N = shape = Y.shape
-    if A.dtype != bf16 or not A.is_cuda or not A.is_contiguous():
+    if A.dtype is not bf16 or not A.is_cuda or not A.is_contiguous():
         _refuse("A", "a contiguous bf16 [adapters][rank][K] on the GPU")
-    if B.shape != (n, N, R) or B.dtype != bf16 or not B.is_cuda or not B.is_contiguous():
+    if B.shape != (n, N, R) or B.dtype is not bf16 or not B.is_cuda or not B.is_contiguous():
         _refuse("B", f"a contiguous bf16 [{n}][{N}][{R}] on the GPU")
-    if X.shape != (M, K) or X.dtype != bf16 or not X.is_cuda or (X.stride(1) != 1 and K > 1):
+    if X.shape != (M, K) or X.dtype is not bf16 or not X.is_cuda or (X.stride(1) != 1 and K > 1):
         _refuse("X", f"bf16 [{M}][{K}] on the GPU, its rows contiguous")
-    if Y.dtype != f32 or not Y.is_cuda or (Y.stride(1) != 1 and N > 1):
+    if Y.dtype is not f32 or not Y.is_cuda or (Y.stride(1) != 1 and N > 1):
         _refuse("Y", "fp32 [tokens][N] on the GPU, its rows contiguous")
     if out is None:
         out = Y
-    elif out.shape != shape or out.dtype != f32 or not out.is_cuda or (out.stride(1) != 1 and N > 1):
+    elif out.shape != shape or out.dtype is not f32 or not out.is_cuda or (out.stride(1) != 1 and N > 1):
         _refuse("out", "fp32 of Y's shape on the GPU, its rows contiguous")
-    if ids.shape != (M,) or ids.dtype != i32 or not ids.is_cuda or not ids.is_contiguous():
+    if ids.shape != (M,) or ids.dtype is not i32 or not ids.is_cuda or not ids.is_contiguous():
         _refuse("ids", f"a contiguous int32 [{M}] on the GPU")
-    if ranks is not None and (ranks.shape != (n,) or ranks.dtype != i32 or not ranks.is_cuda or not ranks.is_contiguous()):
+    if ranks is not None and (ranks.shape != (n,) or ranks.dtype is not i32 or not ranks.is_cuda or not ranks.is_contiguous()):
         _refuse("ranks", f"a contiguous int32 [{n}] on the GPU")
-    if scales is not None and (scales.shape != (n,) or scales.dtype != f32 or not scales.is_cuda or not scales.is_contiguous()):
+    if scales is not None and (scales.shape != (n,) or scales.dtype is not f32 or not scales.is_cuda or not scales.is_contiguous()):
         _refuse("scales", f"a contiguous fp32 [{n}] on the GPU")
     if workspace is None:
         workspace = X.new_empty(max(lqer_adapters_workspace_bytes(M, K, N, R, n), 256), dtype=torch.uint8)
@@ -530,17 +530,21 @@ def lqer_kv4_pool(pages: int, kv_heads: int, page_tokens: int, head_dim: int, de
 
 def _kv4_pool(pool, head_dim, u8):
     """(pages, kv_heads, page_tokens) of a pool for heads of that dimension."""
-    shape = pool.shape
-    if len(shape) != 3 or pool.dtype != u8 or not pool.is_cuda or not pool.is_contiguous():
+    if pool.dim() != 3 or pool.dtype is not u8 or not pool.is_cuda or not pool.is_contiguous():
         _refuse("pool", "a contiguous uint8 [pages][kv_heads][bytes of a page] on the GPU")
-    page_tokens = shape[2] * 8 // (head_dim * 9) if head_dim > 0 else 0
-    if page_tokens * head_dim * 9 != shape[2] * 8:
+    pages, heads, size = pool.shape
+    page_tokens, left = divmod(size * 8, head_dim * 9) if head_dim > 0 else (0, 1)
+    if left:
         _refuse("pool", f"of whole tokens of {head_dim} dimensions")
-    return shape[0], shape[1], page_tokens
+    return pages, heads, page_tokens
 
 
-def _side_by_side(t, heads, head_dim):
-    return t.stride(2) == 1 and (heads == 1 or t.stride(1) == head_dim)
+def _token_stride(stride, tokens, heads, head_dim):
+    """The token stride of [tokens][heads][head_dim] whose heads lie side by side; 0 where they do not."""
+    t, h, d = stride
+    if d != 1 or (h != head_dim and heads != 1):
+        return 0
+    return t if tokens > 1 or t > heads * head_dim else heads * head_dim
 
 
 def lqer_kv4_append(pool, k, v, slots):
@@ -550,46 +554,49 @@ def lqer_kv4_append(pool, k, v, slots):
     T, heads, D = shape = k.shape
     dtype = k.dtype
     pages, pool_heads, P = _kv4_pool(pool, D, torch.uint8)
-    if heads != pool_heads or not k.is_cuda or (dtype != bf16 and dtype != torch.float32) or not _side_by_side(k, heads, D):
-        _refuse("k", f"fp32 or bf16 [tokens][{pool_heads}][head_dim] on the GPU, a token's heads side by side")
-    if v.shape != shape or not v.is_cuda or v.dtype != dtype or not _side_by_side(v, heads, D):
-        _refuse("v", "of k's shape and type, on the GPU, a token's heads side by side")
-    if slots.shape != (T,) or slots.dtype != torch.int32 or not slots.is_cuda or not slots.is_contiguous():
+    if heads != pool_heads or not k.is_cuda or (dtype is not bf16 and dtype is not torch.float32):
+        _refuse("k", f"fp32 or bf16 [tokens][{pool_heads}][head_dim] on the GPU")
+    if v.shape != shape or not v.is_cuda or v.dtype is not dtype:
+        _refuse("v", "of k's shape and type, on the GPU")
+    if slots.shape != (T,) or slots.dtype is not torch.int32 or not slots.is_cuda or not slots.is_contiguous():
         _refuse("slots", f"a contiguous int32 [{T}] on the GPU")
-    st = L.lqer_kv4_append(pool.data_ptr(), pages, P, heads, D, k.data_ptr(), _stride(k, T, heads * D), v.data_ptr(),
-                           _stride(v, T, heads * D), dtype == bf16, T, slots.data_ptr(), _stream())
+    ldk, ldv = _token_stride(k.stride(), T, heads, D), _token_stride(v.stride(), T, heads, D)
+    if not ldk or not ldv:
+        _refuse("k and v", "of heads that lie side by side in a token")
+    st = L.lqer_kv4_append(pool.data_ptr(), pages, P, heads, D, k.data_ptr(), ldk, v.data_ptr(), ldv, dtype is bf16, T, slots.data_ptr(), _stream())
     if st:
         raise LqerError(st, "lqer_kv4_append")
 
 
 @functools.lru_cache(maxsize=256)
 def _kv4_sizes(*sizes):
-    """A call's sizes as the library takes them, and the bytes of its workspace."""
+    """A call's sizes as the library takes them, the bytes of its workspace, and the requests."""
     shape = Kv4Shape(*sizes)
-    return C.byref(shape), int(lib().lqer_kv4_attention_workspace_bytes(C.byref(shape))), shape
+    return C.byref(shape), int(lib().lqer_kv4_attention_workspace_bytes(C.byref(shape))), shape.n_requests
 
 
-def _kv4_shape(pool, q, table, max_q, max_kv, scale, causal, window, out):
-    import torch
-    Tq, q_heads, D = q.shape
+def _kv4_shape(torch, pool, q, table, max_q, max_kv, scale, causal, window, out):
+    Tq, q_heads, D = shape = q.shape
+    bf16 = torch.bfloat16
     pages, heads, P = _kv4_pool(pool, D, torch.uint8)
-    if q.dtype != torch.bfloat16 or not q.is_cuda or not _side_by_side(q, q_heads, D):
+    ldq = _token_stride(q.stride(), Tq, q_heads, D)
+    if not ldq or q.dtype is not bf16 or not q.is_cuda:
         _refuse("q", "bf16 [tokens][q_heads][head_dim] on the GPU, a token's heads side by side")
     ldo, out_type = q_heads * D, 1
     if out is not None:
-        out_type = out.dtype == torch.bfloat16
-        if out.shape != q.shape or not out.is_cuda or (not out_type and out.dtype != torch.float32) or not _side_by_side(out, q_heads, D):
+        ldo, out_type = _token_stride(out.stride(), Tq, q_heads, D) if out.shape == shape else 0, out.dtype is bf16
+        if not ldo or not out.is_cuda or (not out_type and out.dtype is not torch.float32):
             _refuse("out", "bf16 or fp32 of q's shape on the GPU, a token's heads side by side")
-        ldo = _stride(out, Tq, ldo)
-    if table.dim() != 2 or table.dtype != torch.int32 or not table.is_cuda or not table.is_contiguous():
+    if table.dim() != 2 or table.dtype is not torch.int32 or not table.is_cuda or not table.is_contiguous():
         _refuse("table", "a contiguous int32 [requests][pages] on the GPU")
     n, ld = table.shape
-    return _kv4_sizes(n, q_heads, heads, D, P, ld, pages, Tq, _stride(q, Tq, q_heads * D), ldo, max_q, max_kv, bool(causal), window, scale, out_type)
+    return _kv4_sizes(n, q_heads, heads, D, P, ld, pages, Tq, ldq, ldo, max_q, max_kv, bool(causal), window, scale, out_type)
 
 
 def lqer_kv4_attention_workspace_bytes(pool, q, table, max_q: int, max_kv: int, causal: bool = True, window: int = 0) -> int:
     """Bytes of the workspace of lqer_kv4_attention with tensors and numbers like these."""
-    return _kv4_shape(pool, q, table, max_q, max_kv, 1.0, causal, window, None)[1]
+    import torch
+    return _kv4_shape(torch, pool, q, table, max_q, max_kv, 1.0, causal, window, None)[1]
 
 
 def lqer_kv4_attention(pool, q, cu_q, kv_len, table, max_q: int, max_kv: int, scale: float, causal: bool = True, window: int = 0, out=None,
@@ -598,14 +605,13 @@ def lqer_kv4_attention(pool, q, cu_q, kv_len, table, max_q: int, max_kv: int, sc
     and the pages table[b] (int32 tensors).  Returns out (bf16 unless given, bf16 or fp32)."""
     import torch
     L, i32 = _lib or lib(), torch.int32
-    sizes, need, shape = _kv4_shape(pool, q, table, max_q, max_kv, scale, causal, window, out)
-    n = shape.n_requests
-    if cu_q.shape != (n + 1,) or cu_q.dtype != i32 or not cu_q.is_cuda or not cu_q.is_contiguous():
+    sizes, need, n = _kv4_shape(torch, pool, q, table, max_q, max_kv, scale, causal, window, out)
+    if cu_q.shape != (n + 1,) or cu_q.dtype is not i32 or not cu_q.is_cuda or not cu_q.is_contiguous():
         _refuse("cu_q", f"a contiguous int32 [{n + 1}] on the GPU")
-    if kv_len.shape != (n,) or kv_len.dtype != i32 or not kv_len.is_cuda or not kv_len.is_contiguous():
+    if kv_len.shape != (n,) or kv_len.dtype is not i32 or not kv_len.is_cuda or not kv_len.is_contiguous():
         _refuse("kv_len", f"a contiguous int32 [{n}] on the GPU")
     if out is None:
-        out = q.new_empty(q.shape)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if workspace is None and need:
         workspace = q.new_empty(need, dtype=torch.uint8)
     st = L.lqer_kv4_attention(sizes, pool.data_ptr(), q.data_ptr(), cu_q.data_ptr(), kv_len.data_ptr(), table.data_ptr(), out.data_ptr(),

@@ -46,7 +46,7 @@ int lqer_rmsnorm_mx(const void* x_dev, int x_type, int64_t rows, int64_t cols, i
     if (!type_ok(x_type) || !type_ok(weight_type) || (elem_bits != 8 && elem_bits != 6)) return LQER_ERR_UNSUPPORTED;
     const bool res = residual_dev || h_dev;
     if (res && !type_ok(res_type)) return LQER_ERR_UNSUPPORTED;
-    if (rows < 0 || rows > kMaxGrid || cols < 0 || (cols & 15) != 0 || !(eps >= 0.f)) return LQER_ERR_SHAPE;
+    if (rows < 0 || rows > kMaxGrid || cols < 0 || (cols & 15) != 0 || !(eps >= 0.f && eps <= 3.402823466e38f)) return LQER_ERR_SHAPE;
     if (rows == 0 || cols == 0) return LQER_OK;
     if (!x_dev || !weight_dev || !codes_dev || !exps_dev || (res && (!residual_dev || !h_dev))) return LQER_ERR_NULL;
     if (!stride_ok(ldx, cols, x_type) || !aligned(x_dev, 16) || !aligned(weight_dev, 16) || !aligned(codes_dev, 16)) return LQER_ERR_SHAPE;

@@ -27,7 +27,7 @@ def _norm(L, **kw):
     (0, dict(rows=0)), (0, dict(cols=0)), (NULL, dict(x=None)), (NULL, dict(w=None)), (NULL, dict(codes=None)), (NULL, dict(exps=None)),
     (NULL, dict(r=None)), (NULL, dict(h=None)), (UNSUPPORTED, dict(xt=2)), (UNSUPPORTED, dict(rt=-1)), (UNSUPPORTED, dict(wt=7)),
     (UNSUPPORTED, dict(bits=4)), (SHAPE, dict(rows=-1)), (SHAPE, dict(cols=40)), (SHAPE, dict(cols=-16)), (SHAPE, dict(eps=-1.0)),
-    (SHAPE, dict(eps=float("nan"))), (SHAPE, dict(ldx=48)), (SHAPE, dict(ldx=66)), (SHAPE, dict(xt=1, ldx=68)), (SHAPE, dict(ldr=60)),
+    (SHAPE, dict(eps=float("nan"))), (SHAPE, dict(eps=float("inf"))), (SHAPE, dict(ldx=48)), (SHAPE, dict(ldx=66)), (SHAPE, dict(xt=1, ldx=68)), (SHAPE, dict(ldr=60)),
     (SHAPE, dict(ldh=63)), (SHAPE, dict(rt=1, ldh=68)), (SHAPE, dict(ldv=68)), (SHAPE, dict(x=P + 4)), (SHAPE, dict(r=P + 8)),
     (SHAPE, dict(h=P + 8)), (SHAPE, dict(w=P + 4)), (SHAPE, dict(codes=P + 8)), (SHAPE, dict(values=P + 2))])
 def test_norm(L, status, bad):
