@@ -416,9 +416,10 @@ hipError_t launch_d(const Kv4Args& a, hipStream_t s) {
     return join<D, false>(a, s);
 }
 
-// Up to so many cached tokens a workgroup of the kernel for few rows takes all of them, ten steps a wavefront: about as long as parts of one step
-// and the launch that joins them, and one launch less for the host.
-constexpr int64_t kWholeTokens = 1280;
+// Up to so many cached tokens a workgroup of the kernel for few rows takes all of them, five steps a wavefront, ten where the launch has 128 workgroups
+// and more: about as long as parts of one step and the launch that joins them, and one launch less for the host (us in a graph, whole / parts: 517 tokens
+// of 32 heads 12 / 12; 37 requests of up to 1036 tokens 18 / 18; one of 1200 with a single cached head 17 / 12).
+constexpr int64_t kWholeTokens = 640;
 
 // The cached tokens of `lots` tiles cut into parts: `least` tokens at least, and no more than give `wanted` workgroups, all at work at once.
 void cut(Kv4Plan& p, int64_t seen, int64_t lots, int64_t least, int64_t wanted) {
@@ -464,7 +465,7 @@ size_t plan_kv4(Kv4Args& a, void* workspace) {
     // requests' lengths differ many of the 768 have nothing to do (us, 1024 / 768: 16 requests of up to 4096 tokens 24 / 28, all of 4096 30 / 30, 8 of up to
     // 12538 32 / 36; long ones not: 4 of 100003 110 / 103), but not below two steps, which the joining would outweigh (one of 16000 17 / 14).
     const int64_t lots = heads * a.few.row_tiles;
-    if (seen <= kWholeTokens) cut(a.few, seen, lots, seen, 768);
+    if (seen <= (lots >= 128 ? 2 * kWholeTokens : kWholeTokens)) cut(a.few, seen, lots, seen, 768);
     else if (cut(a.few, seen, lots, 128, 768); a.few.chunk <= 1152) cut(a.few, seen, lots, 256, 1024);
     cut(a.many, seen, heads * a.many.row_tiles, 512, 512);
     size_t at = 0;
