@@ -16,7 +16,7 @@
 // exact and the sums are fp32.
 //
 // Measured (projection + second product, us): 16 tokens of 4096 x 4096 rank 16 3.8 + 5.0; 64 of 8192 x 28672 with 48 adapters of up to 64 ranks
-// 7.5 + 24, B's lines at 5.3 TB/s; 203 of 4112 x 11000 5.0 + 7.1, sorting 3.6; 4096 of 8192 x 28672 rank 32 38 + 191, Y at 4.9 TB/s, sorting 8.
+// 7.5 + 24, B's lines at 5.3 TB/s; 203 of 4112 x 11000 5.0 + 7.1, sorting 3.6; 4096 of 8192 x 28672 rank 32 25 + 191, Y at 4.9 TB/s, sorting 8.
 #include "serve.h"
 #include "mx_device.h"
 
@@ -75,12 +75,11 @@ __device__ __forceinline__ int rank_of(const AdapterArgs& a, int adapter) {
     return a.ranks ? min(max(a.ranks[adapter], 0), a.R) : a.R;
 }
 
-// T[split][token][rank]: RT tiles of 16 ranks.  WIDE: each of the four wavefronts has 16 of the tile's 64 tokens; otherwise they share
-// the chunks of K, 16 tokens at a time.
-template <int RT, bool SORTED, bool WIDE>
+// T[split][token][rank]: RT tiles of 16 ranks, up to 16 tokens at a time; the four wavefronts share the chunks of K.
+template <int RT, bool SORTED>
 __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
     __shared__ int rows[kWide];
-    __shared__ f32x4 part[WIDE ? 1 : 4 * RT * 64];
+    __shared__ f32x4 part[4 * RT * 64];
     const Group gr = find_group<SORTED>(a, a.splits, rows);
     const int rank = rank_of(a, gr.adapter);
     if (gr.part >= gr.parts || rank == 0) return;
@@ -88,21 +87,21 @@ __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
     const int64_t per = a.k_split, k_lo = gr.part * per, k_hi = min(a.K, k_lo + per);
     const uint16_t* const A = a.A + (int64_t)gr.adapter * a.R * a.K;
     float* const T = a.T + (int64_t)gr.part * a.M * a.Rp;
-    for (int t0 = WIDE ? 16 * wave : 0; t0 < gr.count; t0 += WIDE ? kWide : 16) {
+    for (int t0 = 0; t0 < gr.count; t0 += 16) {
         const int64_t row = rows[min(t0 + i, gr.count - 1)];
         const uint16_t* const x = a.X + row * a.ldx;
         f32x4 acc[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
         // AHEAD chunks' loads are issued before the first one's products
-        constexpr int AHEAD = RT <= 2 ? 4 : RT == 4 ? 2 : 1, STEP = WIDE ? 64 : 256;
-        for (int64_t k0 = k_lo + (WIDE ? 0 : 64 * wave); k0 < k_hi; k0 += AHEAD * STEP) {
+        constexpr int AHEAD = RT <= 2 ? 4 : RT == 4 ? 2 : 1;
+        for (int64_t k0 = k_lo + 64 * wave; k0 < k_hi; k0 += AHEAD * 256) {
             Frag xf[AHEAD][2], af[AHEAD][2][RT];
 #pragma unroll
             for (int u = 0; u < AHEAD; ++u)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int64_t k = k0 + u * STEP + 16 * g + 8 * h;
+                    const int64_t k = k0 + u * 256 + 16 * g + 8 * h;
                     const bool in = k < k_hi;
                     xf[u][h].u = u32x4{0, 0, 0, 0};
                     if (in) xf[u][h].u = *reinterpret_cast<const u32x4*>(x + k);
@@ -119,23 +118,91 @@ __global__ __launch_bounds__(256) void adapter_project_kernel(AdapterArgs a) {
 #pragma unroll
                     for (int r = 0; r < RT; ++r) acc[r] = mfma16(af[u][h][r].v, xf[u][h].v, acc[r]);
         }
-        if (!WIDE) {                   // the wavefronts' sums, in order
+        // the wavefronts' sums, in order
 #pragma unroll
-            for (int r = 0; r < RT; ++r) part[(wave * RT + r) * 64 + lane] = acc[r];
-            __syncthreads();
-            for (int r = wave; r < RT; r += 4) {
-                f32x4 s = part[r * 64 + lane];
+        for (int r = 0; r < RT; ++r) part[(wave * RT + r) * 64 + lane] = acc[r];
+        __syncthreads();
+        for (int r = wave; r < RT; r += 4) {
+            f32x4 s = part[r * 64 + lane];
 #pragma unroll
-                for (int w = 1; w < 4; ++w) s += part[(w * RT + r) * 64 + lane];
-                if (t0 + i < gr.count && 16 * r + 4 * g < a.Rp) *reinterpret_cast<f32x4*>(T + row * a.Rp + 16 * r + 4 * g) = s;
-            }
-            __syncthreads();
-        } else if (t0 + i < gr.count) {
+            for (int w = 1; w < 4; ++w) s += part[(w * RT + r) * 64 + lane];
+            if (t0 + i < gr.count && 16 * r + 4 * g < a.Rp) *reinterpret_cast<f32x4*>(T + row * a.Rp + 16 * r + 4 * g) = s;
+        }
+        __syncthreads();
+    }
+}
+
+// The same for tiles of 64 tokens, 16 to a wavefront.  Stages of CK values of K go through LDS: neighbouring lanes load neighbouring 16 bytes of a row
+// (the operands' own order, one row a lane, would be the address unit's worst case: 38 us for 4096 tokens of 8192 values and rank 32), and A is
+// read once for all four wavefronts.  The 16-byte cells of row r change places by the low bits of r, off the same banks.
+template <int RT>
+__global__ __launch_bounds__(256) void adapter_project_wide_kernel(AdapterArgs a) {
+    constexpr int CK = RT == 8 ? 64 : 128, C = CK / 8;             // cells of a row
+    constexpr int XN = kWide * C / 256, AN = (16 * RT * C + 255) / 256;
+    __shared__ int rows[kWide];
+    __shared__ u32x4 stage[2][(kWide + 16 * RT) * C];
+    const Group gr = find_group<true>(a, a.splits, rows);
+    const int rank = rank_of(a, gr.adapter);
+    if (gr.part >= gr.parts || rank == 0) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, i = lane & 15, g = lane >> 4;
+    const int64_t k_lo = gr.part * a.k_split, k_hi = min(a.K, k_lo + a.k_split);
+    const int c = tid % C, r0 = tid / C;                           // this thread's cell of the rows r0, r0 + 256 / C ..
+    const uint16_t* const A = a.A + (int64_t)gr.adapter * a.R * a.K + 8 * c;
+    const uint16_t* x[XN];
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
-                if (16 * r + 4 * g < a.Rp) *reinterpret_cast<f32x4*>(T + row * a.Rp + 16 * r + 4 * g) = acc[r];
+    for (int n = 0; n < XN; ++n) x[n] = a.X + rows[min(r0 + n * (256 / C), gr.count - 1)] * a.ldx + 8 * c;
+    u32x4 xv[XN], av[AN];
+    const auto load = [&](int64_t k) {
+        const bool in = k + 8 * c < k_hi;
+#pragma unroll
+        for (int n = 0; n < XN; ++n) {
+            xv[n] = u32x4{0, 0, 0, 0};
+            if (in) xv[n] = *reinterpret_cast<const u32x4*>(x[n] + k);
+        }
+#pragma unroll
+        for (int n = 0; n < AN; ++n) {
+            const int r = r0 + n * (256 / C);
+            av[n] = u32x4{0, 0, 0, 0};
+            if (in && r < rank) av[n] = *reinterpret_cast<const u32x4*>(A + (int64_t)r * a.K + k);
+        }
+    };
+    f32x4 acc[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+    load(k_lo);
+    int buf = 0;
+    for (int64_t k0 = k_lo; k0 < k_hi; k0 += CK, buf ^= 1) {
+        u32x4* const xs = stage[buf];
+        u32x4* const as = stage[buf] + kWide * C;
+#pragma unroll
+        for (int n = 0; n < XN; ++n) {
+            const int r = r0 + n * (256 / C);
+            xs[r * C + (c ^ (r & 7))] = xv[n];
+        }
+#pragma unroll
+        for (int n = 0; n < AN; ++n) {
+            const int r = r0 + n * (256 / C);
+            if (r < 16 * RT) as[r * C + (c ^ (r & 7))] = av[n];
+        }
+        if (k0 + CK < k_hi) load(k0 + CK);
+        __syncthreads();                   // (the other buffer was last read before the barrier of the stage before)
+        if (16 * wave >= gr.count) continue;
+#pragma unroll
+        for (int s = 0; s < CK / 32; ++s) {
+            const int cell = (4 * s + g) ^ (i & 7);
+            Frag xf, af[RT];
+            xf.u = xs[(16 * wave + i) * C + cell];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) af[r].u = as[(16 * r + i) * C + cell];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) acc[r] = mfma16(af[r].v, xf.v, acc[r]);
         }
     }
+    if (16 * wave + i >= gr.count) return;
+    float* const T = a.T + ((int64_t)gr.part * a.M + rows[16 * wave + i]) * a.Rp + 4 * g;
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+        if (16 * r + 4 * g < a.Rp) *reinterpret_cast<f32x4*>(T + 16 * r) = acc[r];
 }
 
 // Y_out = Y_in + T B^T of one group and several blocks of 64 NT output columns; KK steps of 32 ranks.
@@ -394,9 +461,9 @@ int64_t most_groups(const AdapterArgs& a) { return a.tile == 0 ? a.M : a.M / a.t
 template <int RT>
 hipError_t project(const AdapterArgs& a, hipStream_t s) {
     const dim3 grid((unsigned)(most_groups(a) * a.splits));
-    if (a.tile == 0) hipLaunchKernelGGL((adapter_project_kernel<RT, false, false>), grid, dim3(256), 0, s, a);
-    else if (a.tile < kWide) hipLaunchKernelGGL((adapter_project_kernel<RT, true, false>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((adapter_project_kernel<RT, true, true>), grid, dim3(256), 0, s, a);
+    if (a.tile == 0) hipLaunchKernelGGL((adapter_project_kernel<RT, false>), grid, dim3(256), 0, s, a);
+    else if (a.tile < kWide) hipLaunchKernelGGL((adapter_project_kernel<RT, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((adapter_project_wide_kernel<RT>), grid, dim3(256), 0, s, a);
     return hipGetLastError();
 }
 
@@ -431,8 +498,9 @@ hipError_t expand(const AdapterArgs& a, hipStream_t s) {
 size_t plan_adapters(AdapterArgs& a, void* workspace) {
     a.Rp = (a.R + 15) / 16 * 16;
     // Up to 64 tokens need no sorting.  Tiles of 16 tokens, whose four wavefronts share K, as long as they are not many; of 64, which read A and B a quarter
-    // as often, beyond (us, 16 / 64: 251 tokens of 672 x 532 rank 128 16 / 20, 630 of 5696 x 2208 rank 64 23 / 39, 1000 of 4096 x 4096 rank 16 21 / 24;
-    // 1000 of 4096 x 11008 rank 64 with 24 adapters 48 / 44, 1500 of 4096 x 4096 rank 32 27 / 28, 3000 of 2048 x 2048 rank 128 56 / 55).
+    // as often, beyond (us, 16 / 64: 300 tokens of 4096 x 4096 rank 16 14 / 17, 630 of 5696 x 2208 rank 64 23 / 31, 1000 of 672 x 532 rank 128
+    // 18 / 30 and of 4096 x 4096 rank 16 21 / 22; 1000 of 4096 x 11008 rank 64 with 24 adapters 48 / 39, 1500 of 4096 x 4096 rank 32 27 / 25, 3000 of 2048 x 2048
+    // rank 128 56 / 44).
     a.tile = a.M <= kWide ? 0 : a.M <= kNarrowTokens ? 16 : kWide;
     // Parts of K: at least 512 values each, at most 8 parts (that many loads sum T up at once), and with many tokens no more than give two
     // workgroups to a compute unit

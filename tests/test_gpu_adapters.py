@@ -71,6 +71,34 @@ def test_columns(N):
         _check(d, _run(d))
 
 
+# beyond 1024 tokens: tiles of 64, K through LDS in stages of 128 (64 above 64 ranks)
+@pytest.mark.parametrize("R", [8, 16, 24, 40, 72, 128])
+@pytest.mark.parametrize("K", [8, 72, 136, 520, 1032])
+def test_many_tokens(R, K):
+    d = _data(1100, K, 61, R, 5, ldx=K + 8)
+    _check(d, _run(d))
+
+
+@pytest.mark.parametrize("N", [1, 3, 64, 255, 260, 1001])
+def test_many_tokens_columns(N):
+    d = _data(1300, 48, N, 24, 9, ids=[(i // 70) % 10 - 1 for i in range(1300)])
+    _check(d, _run(d))
+    _check(d, _run(d, inplace=True))
+
+
+def test_many_tokens_low_ranks():
+    ranks = [0, 1, 7, 8, 9, 31, 33, 40, 64, 128]
+    d = _data(1500, 200, 90, 128, len(ranks), ranks=ranks)
+    for a, r in enumerate(ranks):
+        d["A"][a, r:] = float("nan")
+        d["B"][a, :, r:] = float("inf")
+    out = _run(d)
+    for a, r in enumerate(ranks):
+        d["A"][a, r:] = 0
+        d["B"][a, :, r:] = 0
+    _check(d, out)
+
+
 def test_many_columns_few_tokens():
     d = _data(48, 128, 7001, 32, 40)             # enough workgroups for the wide instance
     _check(d, _run(d))
