@@ -348,7 +348,7 @@ typedef enum { LQER_F32 = 0, LQER_BF16 = 1 } lqer_type;
  * Root-mean-square norm with the residual's addition, its result as MXINT (Sec. 2.2, block [1,16] of Sec. 4.1):
  *        h = x + residual,   v = h / sqrt(mean(h^2) + eps) * weight,   codes and exponent bytes of v
  *   x_dev         [rows][ldx], x_type;  residual_dev [rows][ldr] and h_dev [rows][ldh], both res_type (h_dev may be
- *                 residual_dev itself); both NULL: h = x, nothing is stored
+ *                 residual_dev itself, ldh = ldr); both NULL: h = x, nothing is stored
  *   weight_dev    [cols], weight_type
  *   cols          multiple of 16; strides in elements, at least cols
  *   elem_bits     8 or 6, codes_dev int8 [rows][cols], exps_dev uint8 [rows][cols/16]: what lqer_linear_forward_q takes

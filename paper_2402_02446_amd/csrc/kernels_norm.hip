@@ -136,7 +136,7 @@ struct Row {
 template <int XT, int RT, int BITS, int STEPS>
 __global__ __launch_bounds__(1024) void rmsnorm_mx_kernel(NormArgs a) {
     __shared__ double part[16];
-    const int64_t row = (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
+    const int64_t row = a.first + (int64_t)blockIdx.x * blockDim.y + threadIdx.y;
     const bool live = row < a.rows;
     const Row<XT, RT, BITS> r{a, row};
     const int64_t stride = (int64_t)blockDim.x * kLane;
@@ -184,8 +184,11 @@ __global__ __launch_bounds__(1024) void rmsnorm_mx_kernel(NormArgs a) {
     }
 }
 
+// A launch counts its threads in 32 bits: so many rows have at most 2^31.
+constexpr int64_t kRowsAtOnce = 1 << 21;
+
 template <int XT, int RT, int BITS>
-hipError_t launch(const NormArgs& a, hipStream_t s) {
+hipError_t launch(NormArgs a, hipStream_t s) {
     const int64_t units = a.cols / kLane;
     int tx, ty = 1, steps;
     if (units <= 128) { tx = 64; ty = 4; }
@@ -193,12 +196,17 @@ hipError_t launch(const NormArgs& a, hipStream_t s) {
     else if (units <= 2048) { tx = 512; }
     else { tx = 1024; }
     steps = (int)((units + tx - 1) / tx);
-    const dim3 grid((unsigned)((a.rows + ty - 1) / ty)), block(tx, ty);
-    if (steps <= 1) hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 1>), grid, block, 0, s, a);
-    else if (steps <= 2) hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 2>), grid, block, 0, s, a);
-    else if (steps <= 4) hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 4>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 0>), grid, block, 0, s, a);
-    return hipGetLastError();
+    const dim3 block(tx, ty);
+    for (; a.first < a.rows; a.first += kRowsAtOnce) {
+        const int64_t rows = a.rows - a.first < kRowsAtOnce ? a.rows - a.first : kRowsAtOnce;
+        const dim3 grid((unsigned)((rows + ty - 1) / ty));
+        if (steps <= 1) hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 1>), grid, block, 0, s, a);
+        else if (steps <= 2) hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 2>), grid, block, 0, s, a);
+        else if (steps <= 4) hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 4>), grid, block, 0, s, a);
+        else hipLaunchKernelGGL((rmsnorm_mx_kernel<XT, RT, BITS, 0>), grid, block, 0, s, a);
+        if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 template <int XT, int RT>

@@ -19,6 +19,7 @@ struct NormArgs {
     int8_t* codes;
     uint8_t* exps;
     uint16_t* values;              // may be null
+    int64_t first;                 // set by launch_rmsnorm_mx: the launch's first row
 };
 hipError_t launch_rmsnorm_mx(const NormArgs& a, hipStream_t s);
 

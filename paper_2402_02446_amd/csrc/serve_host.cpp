@@ -52,9 +52,10 @@ int lqer_rmsnorm_mx(const void* x_dev, int x_type, int64_t rows, int64_t cols, i
     if (!stride_ok(ldx, cols, x_type) || !aligned(x_dev, 16) || !aligned(weight_dev, 16) || !aligned(codes_dev, 16)) return LQER_ERR_SHAPE;
     if (res && (!stride_ok(ldr, cols, res_type) || !stride_ok(ldh, cols, res_type) || !aligned(residual_dev, 16) || !aligned(h_dev, 16)))
         return LQER_ERR_SHAPE;
+    if (res && residual_dev == h_dev && ldr != ldh) return LQER_ERR_SHAPE;
     if (values_dev && (!stride_ok(ldv, cols, LQER_BF16) || !aligned(values_dev, 16))) return LQER_ERR_SHAPE;
     const NormArgs a{x_dev, residual_dev, h_dev, weight_dev, x_type, res_type, weight_type, rows, cols, ldx, ldr, ldh, ldv, eps, elem_bits,
-                     codes_dev, exps_dev, values_dev};
+                     codes_dev, exps_dev, values_dev, 0};
     return launch_rmsnorm_mx(a, (hipStream_t)hip_stream) == hipSuccess ? LQER_OK : LQER_ERR_HIP;
 }
 

@@ -34,6 +34,12 @@ def test_norm(L, status, bad):
     assert _norm(L, **bad) == status
 
 
+# the residual updated in place is one array with one stride
+@pytest.mark.parametrize("ldr, ldh", [(64, 128), (96, 64)])
+def test_norm_in_place_strides(L, ldr, ldh):
+    assert _norm(L, r=P, h=P, ldr=ldr, ldh=ldh) == SHAPE
+
+
 def _adapters(L, **kw):
     a = dict(X=P, M=4, K=64, ldx=64, ids=P, A=P, B=P, n=3, R=16, ranks=P, scales=P, yi=P, ldyi=40, yo=P, N=40, ldyo=40, ws=P, bytes=1 << 20)
     a.update(kw)

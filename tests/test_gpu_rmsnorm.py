@@ -94,6 +94,21 @@ def test_no_rows():
     assert codes.shape == (0, 64) and exps.shape == (0, 4) and h is None and v is None
 
 
+def test_more_rows_than_a_launch_has_threads_for():
+    import torch
+    from paper_2402_02446_amd import binding
+    rows = (1 << 26) + 5                         # 64 threads a row: 2^32 and a few
+    x = torch.randn(rows, 16, device="cuda", dtype=torch.bfloat16)
+    w = torch.rand(16, device="cuda") + 0.5
+    codes, exps, _, _ = binding.lqer_rmsnorm_mx(x, w, 1e-5)
+    for at in (0, (1 << 21) - 500, (1 << 25) - 500, rows - 1000):
+        c, e, _, _ = binding.lqer_rmsnorm_mx(x[at:at + 1000], w, 1e-5)
+        assert torch.equal(codes[at:at + 1000], c) and torch.equal(exps[at:at + 1000], e)
+        v = block.rmsnorm(x[at:at + 1000].double().cpu().numpy(), w.double().cpu().numpy(), float(np.float32(1e-5)))
+        oc, oe = mxint.mx_quantize(v, 8)
+        assert np.array_equal(c.cpu().numpy(), oc) and np.array_equal(e.cpu().numpy(), oe)
+
+
 def test_feeds_the_linear():
     """Codes of the norm through lqer_linear_forward_q are the bits of its values through lqer_linear_forward."""
     import torch
