@@ -58,6 +58,11 @@ def test_adapters(L, status, bad):
     assert _adapters(L, **bad) == status
 
 
+def test_adapters_tokens(L):
+    assert _adapters(L, M=(1 << 29) + 1) == SHAPE and L.lqer_adapters_workspace_bytes((1 << 29) + 1, 64, 40, 16, 3) == 0
+    assert _adapters(L, M=1 << 29) == WORKSPACE and L.lqer_adapters_workspace_bytes(1 << 29, 64, 40, 16, 3) > 1 << 35
+
+
 def test_adapters_workspace(L):
     need = L.lqer_adapters_workspace_bytes(4, 64, 40, 16, 3)
     assert need > 0 and _adapters(L, bytes=need - 1) == WORKSPACE
