@@ -506,6 +506,8 @@ def lqer_adapters_forward(X, ids, A, B, Y, out=None, ranks=None, scales=None, wo
         _refuse("scales", f"a contiguous fp32 [{n}] on the GPU")
     if workspace is None:
         workspace = X.new_empty(max(lqer_adapters_workspace_bytes(M, K, N, R, n), 256), dtype=torch.uint8)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        _refuse("workspace", "contiguous, on the GPU")
     st = L.lqer_adapters_forward(X.data_ptr(), M, K, _stride(X, M, K), ids.data_ptr(), A.data_ptr(), B.data_ptr(), n, R,
                                  None if ranks is None else ranks.data_ptr(), None if scales is None else scales.data_ptr(),
                                  Y.data_ptr(), _stride(Y, M, N), out.data_ptr(), N, _stride(out, M, N),
@@ -612,8 +614,11 @@ def lqer_kv4_attention(pool, q, cu_q, kv_len, table, max_q: int, max_kv: int, sc
         _refuse("kv_len", f"a contiguous int32 [{n}] on the GPU")
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    if workspace is None and need:
-        workspace = q.new_empty(need, dtype=torch.uint8)
+    if workspace is None:
+        if need:
+            workspace = q.new_empty(need, dtype=torch.uint8)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        _refuse("workspace", "contiguous, on the GPU")
     st = L.lqer_kv4_attention(sizes, pool.data_ptr(), q.data_ptr(), cu_q.data_ptr(), kv_len.data_ptr(), table.data_ptr(), out.data_ptr(),
                               None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.nbytes, _stream())
     if st:

@@ -194,3 +194,13 @@ def test_tensors_that_the_library_cannot_check():
                 dict(Y=a["Y"].cpu()), dict(X=a["X"][:, ::2])):
         with pytest.raises(ValueError):
             binding.lqer_adapters_forward(**{**a, **bad})
+
+
+def test_a_workspace_of_its_own_is_contiguous_and_on_the_gpu():
+    import torch
+    from paper_2402_02446_amd import binding
+    d = _data(4, 64, 32, 16, 2)
+    a = {k: d[k].cuda() for k in ("X", "ids", "A", "B", "Y", "ranks", "scales")}
+    for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(256, dtype=torch.uint8, device="cuda")[:, None].expand(256, 4096)):
+        with pytest.raises(ValueError):
+            binding.lqer_adapters_forward(**a, workspace=bad)

@@ -330,3 +330,14 @@ def test_tensors_that_the_library_cannot_check():
         binding.lqer_kv4_attention(**{**a, "q": torch.zeros(1, 3, 64, dtype=torch.bfloat16, device="cuda")})
     with pytest.raises(binding.LqerError):
         binding.lqer_kv4_pool(4, 2, 24, 64)
+
+
+def test_a_workspace_of_its_own_is_contiguous_and_on_the_gpu():
+    import torch
+    from paper_2402_02446_amd import binding
+    pool = binding.lqer_kv4_pool(4, 2, 16, 64)
+    q = torch.zeros(1, 4, 64, dtype=torch.bfloat16, device="cuda")
+    i = torch.ones(2, dtype=torch.int32, device="cuda")
+    for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(256, dtype=torch.uint8, device="cuda")[:, None].expand(256, 4096)):
+        with pytest.raises(ValueError):
+            binding.lqer_kv4_attention(pool, q, i, i[:1], i[None], 1, 4000, 1.0, workspace=bad)
