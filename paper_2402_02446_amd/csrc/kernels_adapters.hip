@@ -336,7 +336,7 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
             if (tt == 0) {
                 now = next;
                 now.cut(rank, g);
-                const bool more = c + 1 < columns;
+                const bool more = c + 1 < columns && n0 + 64 * NT < a.N;       // (the last workgroups' share may end before)
                 if (more || t0 + TROWS < gr.count) next.load(a, B, more ? n0 + 64 * NT : first, rank, i, g);
             }
             FourRows<NT> y = y_next;

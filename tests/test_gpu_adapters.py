@@ -204,3 +204,14 @@ def test_a_workspace_of_its_own_is_contiguous_and_on_the_gpu():
     for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(256, dtype=torch.uint8, device="cuda")[:, None].expand(256, 4096)):
         with pytest.raises(ValueError):
             binding.lqer_adapters_forward(**a, workspace=bad)
+
+
+# Up to 64 tokens, more than 16 of them with one adapter, several blocks of columns to a workgroup and fewer to the last one or to its last
+# wavefronts: B of the first block is read again for the next 16 tokens.  (ranks: 32, 64 and 128 at most)
+@pytest.mark.parametrize("R", [16, 40, 128])
+@pytest.mark.parametrize("N, groups, one", [(7001, 19, 46), (28672, 10, 55), (11008, 24, 41), (14336, 19, 30)])
+def test_one_adapter_of_many_tokens_beside_others(R, N, groups, one):
+    rng = np.random.default_rng(N + R)
+    d = _data(one + groups - 1, 40, N, R, groups, ids=rng.permutation([groups - 1] * one + list(range(groups - 1))))
+    _check(d, _run(d))
+    _check(d, _run(d, inplace=True))
