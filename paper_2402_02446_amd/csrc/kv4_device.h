@@ -41,7 +41,7 @@ __device__ __forceinline__ int kv4_row_end(const Kv4Args& a, const Kv4Rows& r, i
     return a.sh.causal ? min(max(r.position(i) + 1, 0), r.len) : r.len;
 }
 __device__ __forceinline__ int kv4_row_begin(const Kv4Args& a, const Kv4Rows& r, int i) {
-    return a.sh.window > 0 ? max((int)min((int64_t)r.position(i) - a.sh.window + 1, (int64_t)r.len), 0) : 0;
+    return a.sh.window > 0 ? (int)min(max((int64_t)r.position(i) - a.sh.window + 1, (int64_t)0), (int64_t)r.len) : 0;
 }
 
 __device__ __forceinline__ void kv4_tile(const Kv4Args& a, Kv4Rows& r, int row0, int most) {

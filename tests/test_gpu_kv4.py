@@ -341,3 +341,10 @@ def test_a_workspace_of_its_own_is_contiguous_and_on_the_gpu():
     for bad in (torch.empty(1 << 20, dtype=torch.uint8), torch.empty(256, dtype=torch.uint8, device="cuda")[:, None].expand(256, 4096)):
         with pytest.raises(ValueError):
             binding.lqer_kv4_attention(pool, q, i, i[:1], i[None], 1, 4000, 1.0, workspace=bad)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 12])
+def test_windows_as_wide_as_the_type(window):
+    """A query before the cache's beginning: its window begins below -2^31."""
+    _attend([21, 1], [18, 30], 4, 2, 64, 16, window=window)
+    _attend([25, 90], [3, 40], 4, 2, 128, 16, causal=False, window=window)
