@@ -574,6 +574,10 @@ def lqer_kv4_append(pool, k, v, slots):
 def _kv4_sizes(*sizes):
     """A call's sizes as the library takes them, the bytes of its workspace, and the requests."""
     shape = Kv4Shape(*sizes)
+    max_q, max_kv, _, window = sizes[10:14]
+    if not (0 <= max_q < 1 << 31 and 0 <= max_kv < 1 << 31 and 0 <= window < 1 << 31):
+        # (ctypes keeps the low 32 bits: a wide window would be a narrow one)
+        shape.max_q, shape.max_kv, shape.window = (min(max(n, -1), (1 << 31) - 1) for n in (max_q, max_kv, window))
     return C.byref(shape), int(lib().lqer_kv4_attention_workspace_bytes(C.byref(shape))), shape.n_requests
 
 

@@ -130,3 +130,12 @@ def test_kv4_attention_workspace(L):
 def test_kv4_attention_without_a_shape(L):
     assert L.lqer_kv4_attention(None, P, P, P, P, P, P, P, 0, None) == NULL
     assert L.lqer_kv4_attention_workspace_bytes(None) == 0
+
+
+@pytest.mark.parametrize("name", ["max_q", "max_kv", "window"])
+def test_kv4_numbers_beyond_32_bits(L, name):
+    """A caller's estimates and window are taken as the largest that the library takes, a negative one stays negative."""
+    a = dict(n_requests=2, q_heads=8, kv_heads=2, head_dim=64, page_tokens=16, table_ld=400, pages=900, Tq=2, ldq=512, ldo=512, max_q=1, max_kv=6000,
+             causal=True, window=0, scale=0.125, out_type=True)
+    for value, taken in ((2 ** 31 - 1, 2 ** 31 - 1), (2 ** 32 + 1, 2 ** 31 - 1), (2 ** 63, 2 ** 31 - 1), (-2 ** 32 + 1, -1), (3, 3)):
+        assert getattr(binding._kv4_sizes(*{**a, name: value}.values())[0]._obj, name) == taken
