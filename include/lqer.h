@@ -420,7 +420,8 @@ int lqer_kv4_append(uint8_t* pool_dev, int64_t pages, int page_tokens, int kv_he
  * Request b has the queries cu_q[b] .. cu_q[b+1]-1 and kv_len[b] cached tokens, n = cu_q[b+1] - cu_q[b] of which are
  * the queries' own: query i stands at position p = kv_len[b] - n + i and sees t <= p (causal; t < kv_len[b] otherwise),
  * and with window > 0 only t > p - window.  A query that sees nothing has the output 0.
- *   q_dev       bf16 [Tq][q_heads][head_dim], token stride ldq (multiple of 8), 16-byte aligned
+ *   q_dev       bf16 [Tq][q_heads][head_dim], token stride ldq (multiple of 8), 16-byte aligned; finite (a NaN comes out as NaN, in its
+ *               own query's row and head alone)
  *   cu_q_dev    int32 [n_requests + 1], kv_len_dev int32 [n_requests]
  *   table_dev   int32 [n_requests][table_ld]: page of tokens 0 .. P-1, P .. 2P-1, ..; kv_len is taken as at most
  *               table_ld * P; a page outside the pool: its tokens are not seen

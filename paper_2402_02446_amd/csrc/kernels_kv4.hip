@@ -291,13 +291,13 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 ? 3 : 2) void kv4_few_k
             for (int w = 1; w < WAVES; ++w) top = __builtin_fmaxf(top, join_m[w][c]);
             f32x4 sum = {0.f, 0.f, 0.f, 0.f};
             float weights = 0.f;
-            if (top > -__builtin_inff())
+            // (nothing seen: sums of 0; scores of NaN alone leave no maximum either, and sums of NaN)
 #pragma unroll
-                for (int w = 0; w < WAVES; ++w) {
-                    const float f = exp2_fast(join_m[w][c] - top);
-                    weights += f * join_l[w][c];
-                    sum += f * *reinterpret_cast<const f32x4*>(&join_o[w][c][d]);
-                }
+            for (int w = 0; w < WAVES; ++w) {
+                const float f = top > -__builtin_inff() ? exp2_fast(join_m[w][c] - top) : 1.0f;
+                weights += f * join_l[w][c];
+                sum += f * *reinterpret_cast<const f32x4*>(&join_o[w][c][d]);
+            }
             const int rr = r.row0 + c, qu = rr / a.group;
             const int64_t orow = r.first + qu;
             const int h = head * a.group + rr - qu * a.group;

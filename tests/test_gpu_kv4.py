@@ -348,3 +348,29 @@ def test_windows_as_wide_as_the_type(window):
     """A query before the cache's beginning: its window begins below -2^31."""
     _attend([21, 1], [18, 30], 4, 2, 64, 16, window=window)
     _attend([25, 90], [3, 40], 4, 2, 128, 16, causal=False, window=window)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), -float("inf")])
+@pytest.mark.parametrize("tokens, n", [(40, 1), (700, 2), (4000, 1), (300, 40), (3000, 40)])
+def test_a_query_that_is_not_finite_spoils_itself_only(bad, tokens, n):
+    """Its scores are NaN wherever a key has a zero there, and so is the softmax over them; the other rows keep their bits."""
+    import torch
+    from paper_2402_02446_amd import binding
+    D, P, heads, G = 128, 16, 2, 4
+    g = torch.Generator().manual_seed(tokens + n)
+    pages = -(-tokens // P)
+    pool = binding.lqer_kv4_pool(pages, heads, P, D)
+    k, v = (torch.randn(tokens, heads, D, generator=g) for _ in range(2))
+    k[:, :, 5] = 0
+    v[::3] = 0                                      # (NaN times 0)
+    binding.lqer_kv4_append(pool, k.cuda(), v.cuda(), torch.arange(tokens, dtype=torch.int32, device="cuda"))
+    q = torch.randn(n, heads * G, D, generator=g).bfloat16().cuda()
+    i32 = lambda *x: torch.tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    table = torch.arange(pages, dtype=torch.int32, device="cuda")[None]
+    call = lambda: binding.lqer_kv4_attention(pool, q, i32(0, n), i32(tokens), table, n, tokens, D ** -0.5)  # noqa: E731
+    want = call()
+    q[n // 2, 6, 5] = bad
+    got = call()
+    assert bool(torch.isnan(got[n // 2, 6]).all())
+    got[n // 2, 6] = want[n // 2, 6]
+    assert torch.equal(got, want)
