@@ -431,7 +431,8 @@ int lqer_kv4_append(uint8_t* pool_dev, int64_t pages, int page_tokens, int kv_he
  *   workspace_dev  lqer_kv4_attention_workspace_bytes(...) of the same numbers, 256-byte aligned, scratch
  * q_heads is a multiple of kv_heads.  Scores, running maxima, sums and outputs are fp32; the weights exp(s - max) enter the product
  * with V as two bf16 terms (relative 2^-16) where a request has up to 64 rows (queries times query heads of a cached head), as one (2^-8 at
- * most) where it has more: prompts are bound by the matrix instructions.
+ * most) where it has more: prompts are bound by the matrix instructions.  Only a request that is alone in its call is taken by max_q there,
+ * where q has as many rows, not by its length.
  */
 typedef struct {
     int n_requests;

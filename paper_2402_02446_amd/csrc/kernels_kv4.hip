@@ -449,11 +449,12 @@ size_t plan_kv4(Kv4Args& a, void* workspace) {
     a.few_rows = kFewRows;
     const int64_t rows = (int64_t)sh.max_q * a.group, most_tiles = 65535 / sh.kv_heads;
     const auto tiles = [&](int64_t n, int64_t of) { return (int)std::max<int64_t>(1, std::min<int64_t>((n + of - 1) / of, most_tiles)); };
-    // Requests of few rows beside ones of many: only where some are shorter than the longest.
     a.many = Kv4Plan{};
     a.few = Kv4Plan{};
     a.many.run = rows > kFewRows;
-    a.few.run = !a.many.run || sh.Tq < (int64_t)sh.n_requests * sh.max_q;
+    // Beside the kernel for many rows the one for few runs whenever some request may have few: the lengths are on the device, Tq counts rows that no request
+    // has, and max_q is an estimate.  (A single request is taken to be as long as max_q says, unless q has not so many rows.)
+    a.few.run = !a.many.run || sh.n_requests > 1 || sh.Tq < sh.max_q;
     a.many.row_tiles = tiles(rows, kManyRows);
     a.few.cap = (int)std::max<int64_t>(1, std::min<int64_t>(rows, kFewRows));
     a.few.row_tiles = tiles(a.few.cap, 16);
