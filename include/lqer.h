@@ -379,7 +379,7 @@ int lqer_rmsnorm_mx(const void* x_dev, int x_type, int64_t rows, int64_t cols, i
  *   Y_in_dev   fp32 [M][ldyi], Y_out_dev fp32 [M][ldyo]; the same array (rows without an adapter are then left alone)
  *              or two that do not overlap; N is any number, ldyi, ldyo >= N and multiples of 4
  * Pointers 16-byte aligned (ids, ranks, scales: 4).  Products are exact, sums fp32; the projection X A^T enters the second
- * product in three bf16 terms, its whole 24 bits.  n_adapters at most 8192 (LQER_ERR_UNSUPPORTED), M at most
+ * product in three bf16 terms, its whole 24 bits.  Where it is infinite or NaN, Y_out is as the formula has it; B must be finite.  n_adapters at most 8192 (LQER_ERR_UNSUPPORTED), M at most
  * 2^29, N at most 2^22 - 64 (LQER_ERR_SHAPE).
  * workspace_dev: at least lqer_adapters_workspace_bytes(M, K, N, R, n_adapters) bytes, 256-byte aligned, scratch.
  */

@@ -313,11 +313,11 @@ __global__ __launch_bounds__(256) void adapter_expand_kernel(AdapterArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const float f = r + j < rank ? v[j] * scale : 0.f;
-                    const __bf16 t1 = (__bf16)f;
-                    const float f2 = f - (float)t1;
-                    const __bf16 t2 = (__bf16)f2;
-                    const __bf16 t3 = (__bf16)(f2 - (float)t2);
-                    const uint32_t u[3] = {__builtin_bit_cast(uint16_t, t1), __builtin_bit_cast(uint16_t, t2), __builtin_bit_cast(uint16_t, t3)};
+                    // cut off after 8 bits each, which is as exact as rounding and never rounds to infinity; an infinity has no rest
+                    const float t1 = f32_from_bits(f32_bits(f) & 0xFFFF0000u);
+                    const float f2 = __builtin_fabsf(f) < __builtin_inff() ? f - t1 : 0.f;
+                    const float t2 = f32_from_bits(f32_bits(f2) & 0xFFFF0000u);
+                    const uint32_t u[3] = {f32_bits(t1) >> 16, f32_bits(t2) >> 16, f32_bits(f2 - t2) >> 16};
 #pragma unroll
                     for (int q = 0; q < 3; ++q) w[q][j >> 1] = j & 1 ? w[q][j >> 1] | u[q] << 16 : u[q];
                 }

@@ -215,3 +215,29 @@ def test_one_adapter_of_many_tokens_beside_others(R, N, groups, one):
     d = _data(one + groups - 1, 40, N, R, groups, ids=rng.permutation([groups - 1] * one + list(range(groups - 1))))
     _check(d, _run(d))
     _check(d, _run(d, inplace=True))
+
+
+@pytest.mark.parametrize("M", [5, 100, 1100])
+def test_numbers_that_are_not_finite_or_close_to_it(M):
+    """T = X A^T infinite, NaN, or between the largest bf16 and the largest fp32 number: Y is what the formula gives."""
+    d = _data(M, 64, 70, 16, 2, ids=[0] * M, ranks=[9, 16])
+    d["A"][:], d["X"][:], d["B"][:] = 0, 0, 0
+    for r in range(9):
+        d["A"][0, r, r] = 1
+        d["B"][0, :, r] = 1
+    d["A"][0, :9, 20] = 2
+    d["B"][0, 40:, 3] = 2.0 ** -100
+    d["X"][:, 3] = 3.0
+    d["X"][1, 20] = float("inf")                    # T infinite in every rank
+    d["X"][2, 20] = -float("inf")
+    d["X"][3, 20] = float("nan")
+    big = 2.0 ** 127 * (2 - 2.0 ** -7)              # the largest bf16 number; half a unit more would round to infinity
+    d["X"][4, 3], d["A"][0, 3, 30], d["X"][4, 30] = big, 1, 2.0 ** 119 * 1.5
+    d["scales"][:] = 1
+    out = _run(d).double().cpu().numpy()
+    assert np.all(out[1] == np.inf) and np.all(out[2] == -np.inf) and np.all(np.isnan(out[3]))
+    rest = [m for m in range(M) if m not in (1, 2, 3)]
+    ref, mag = block.adapters(d["X"][rest].double().numpy(), np.zeros(len(rest)), d["A"].double().numpy(), d["B"].double().numpy(),
+                              d["Y"][rest].double().numpy(), d["ranks"].numpy(), d["scales"].numpy())
+    assert ref[4 - 3].max() > big                   # (token 4)
+    assert np.all(np.abs(out[rest] - ref) <= 4 * U32 * (mag + np.abs(ref)))
