@@ -5,8 +5,8 @@
 // bounds them: with few tokens the bytes of the A and B of the adapters in the batch, each read by one group; with many the
 // bytes of X and of Y in and out.
 //
-// Groups.  Up to 64 tokens a wavefront of every workgroup finds the groups that there are by itself: of the tokens with one adapter one finds its own
-// number in a table in LDS; the workgroups are shared out among the groups.  Beyond, one workgroup sorts the tokens by adapter first
+// Groups.  Up to 64 tokens a wavefront of every workgroup finds the groups that there are by itself, through a table in LDS; the workgroups are shared out
+// among the groups.  Beyond, one workgroup sorts the tokens by adapter first
 // and lists tiles of up to 16 or 64 of them.  Tokens without an adapter are a group of rank 0: their rows are copied.
 //
 // Matrix instructions: 16 x 16 x 32 bf16.  Projection: ranks as rows and tokens as columns, so that a lane holds four neighbouring ranks
@@ -38,6 +38,12 @@ __device__ __forceinline__ int adapter_of(const AdapterArgs& a, int64_t m) {
     return id >= 0 && id < a.n ? id : -1;
 }
 
+// What the lanes of a wavefront stored in LDS before is there for all of them.
+__device__ __forceinline__ void wave_sync() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // What this workgroup works on, and its group's tokens in rows[] (LDS).  Uniform over the workgroup; holds barriers.
 // Without sorting, parts = 0: all workgroups are shared out evenly among the groups that there are; otherwise `parts` to each group or tile.
 template <bool SORTED>
@@ -45,13 +51,20 @@ __device__ __forceinline__ Group find_group(const AdapterArgs& a, int parts, int
     __shared__ Group found;
     if (!SORTED) {
         __shared__ uint8_t seen[kMaxAdapters + 1];
+        __shared__ int lowest[kWide];
         if (threadIdx.x < 64) {
             const int lane = threadIdx.x;
             const bool in = lane < a.M;
             const int id = in ? adapter_of(a, lane) : -2, at = id < 0 ? a.n : id;
-            // of the tokens of an adapter one finds its own number there: any one of them will do
-            if (in) *(volatile uint8_t*)&seen[at] = (uint8_t)lane;
-            const uint64_t firsts = __ballot(in && *(volatile uint8_t*)&seen[at] == lane);
+            // The tokens of an adapter find one and the same of them in the table, whichever that is; the lowest of those that found it leads the group, so that the
+            // groups have the same order in every workgroup.
+            lowest[lane] = kWide;
+            if (in) __hip_atomic_store(&seen[at], (uint8_t)lane, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+            wave_sync();
+            const int met = in ? __hip_atomic_load(&seen[at], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP) : 0;
+            if (in) atomicMin(&lowest[met], lane);
+            wave_sync();
+            const uint64_t firsts = __ballot(in && lowest[met] == lane);
             const int groups = (int)__popcll(firsts);
             const bool mine = ((firsts >> lane) & 1) && (int)__popcll(firsts & ((1ull << lane) - 1)) == (int)(blockIdx.x % groups);
             const int adapter = __builtin_amdgcn_readlane(id, (int)__builtin_ctzll(__ballot(mine)));

@@ -241,3 +241,14 @@ def test_numbers_that_are_not_finite_or_close_to_it(M):
                               d["Y"][rest].double().numpy(), d["ranks"].numpy(), d["scales"].numpy())
     assert ref[4 - 3].max() > big                   # (token 4)
     assert np.all(np.abs(out[rest] - ref) <= 4 * U32 * (mag + np.abs(ref)))
+
+
+# Every token's group is found by every workgroup alike, whatever the mix of adapters: no token is left out, none counted twice (in place).
+@pytest.mark.parametrize("M", [2, 7, 16, 41, 64])
+def test_mixes_of_adapters(M):
+    rng = np.random.default_rng(M)
+    for most in (1, 2, 3, 5, 9, 20, 64, 8192):
+        ids = rng.integers(-1, most, M)
+        ids[rng.integers(0, M, M // 3)] = ids[0]
+        d = _data(M, 24, 140, 8, min(most, 300), ids=np.where(ids >= 300, ids % 300, ids))
+        _check(d, _run(d, inplace=True))
