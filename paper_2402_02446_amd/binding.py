@@ -437,8 +437,8 @@ def _refuse(name, what):
 
 
 def _stride(t, rows, cols):
-    """The row stride of a matrix; a single row has none of its own."""
-    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    """The row stride of a matrix; a single row has none of its own, and goes by one that the library takes."""
+    return t.stride(0) if rows > 1 else (cols + 7) & -8
 
 
 def lqer_rmsnorm_mx(x, weight, eps: float = 1e-5, residual=None, h_out=None, elem_bits: int = 8, values: bool = False):
@@ -546,7 +546,7 @@ def _token_stride(stride, tokens, heads, head_dim):
     t, h, d = stride
     if d != 1 or (h != head_dim and heads != 1):
         return 0
-    return t if tokens > 1 or t > heads * head_dim else heads * head_dim
+    return t if tokens > 1 else heads * head_dim
 
 
 def lqer_kv4_append(pool, k, v, slots):

@@ -139,3 +139,18 @@ def test_kv4_numbers_beyond_32_bits(L, name):
              causal=True, window=0, scale=0.125, out_type=True)
     for value, taken in ((2 ** 31 - 1, 2 ** 31 - 1), (2 ** 32 + 1, 2 ** 31 - 1), (2 ** 63, 2 ** 31 - 1), (-2 ** 32 + 1, -1), (3, 3)):
         assert getattr(binding._kv4_sizes(*{**a, name: value}.values())[0]._obj, name) == taken
+
+
+@pytest.mark.parametrize("rows", [0, 1])
+def test_a_single_row_has_no_stride_of_its_own(rows):
+    """What torch says of it, as a slice of a wider buffer or of an odd width, is not what a row has to keep to."""
+    import torch
+    for width, cols in ((4100, 4096), (4099, 4096), (203, 203), (8, 8), (1, 1)):
+        got = binding._stride(torch.empty(3, width)[:rows, :cols], rows, cols)
+        assert got >= cols and got % 8 == 0
+    for heads, D, buffer in ((2, 64, (3, 2, 65)), (4, 128, (3, 7, 128)), (1, 64, (3, 1, 70)), (1, 256, (3, 5, 257))):
+        t = torch.empty(buffer)[:rows, :heads, :D]
+        if heads == 1 or t.stride(1) == D:
+            assert binding._token_stride(t.stride(), rows, heads, D) == heads * D
+        else:
+            assert binding._token_stride(t.stride(), rows, heads, D) == 0

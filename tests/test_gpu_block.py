@@ -92,3 +92,25 @@ def test_prompts_then_tokens(example):
 def test_the_example_runs(example, capsys):
     example.main()
     assert "decode steps of 3 requests" in capsys.readouterr().out
+
+
+def test_one_token_out_of_wider_buffers():
+    """A single row out of a buffer whose rows start anywhere: the same bits as a contiguous one."""
+    import torch
+    from paper_2402_02446_amd import binding as lqer
+    odd = lambda t: torch.cat([t, t[:, :3]], 1)[:, : t.shape[1]] if t.dim() == 2 else torch.cat([t.flatten(1), t.flatten(1)[:, :3]], 1)[:, : t[0].numel()].view(t.shape)  # noqa: E731
+    same = lambda a, b: all((x is None and y is None) or torch.equal(x, y) for x, y in zip(a, b))  # noqa: E731
+    for dtype in (torch.float32, torch.bfloat16):
+        x, r, w = torch.randn(1, 4096, device="cuda", dtype=dtype), torch.randn(1, 4096, device="cuda", dtype=dtype), torch.rand(4096, device="cuda")
+        assert odd(x).stride(0) == 4099
+        assert same(lqer.lqer_rmsnorm_mx(odd(x), w, residual=odd(r), values=True), lqer.lqer_rmsnorm_mx(x, w, residual=r, values=True))
+    X, A, B = (torch.randn(*s, device="cuda").bfloat16() for s in ((1, 512), (2, 16, 512), (2, 203, 16)))
+    Y, ids = torch.randn(1, 204, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    want = lqer.lqer_adapters_forward(X, ids, A, B, Y[:, :203], out=torch.empty(1, 204, device="cuda")[:, :203])
+    assert torch.equal(lqer.lqer_adapters_forward(odd(X), ids, A, B, Y[:, :203].contiguous()), want)
+    pool, q = lqer.lqer_kv4_pool(4, 1, 16, 64), torch.randn(1, 2, 64, device="cuda").bfloat16()
+    k, v = (torch.randn(1, 1, 64, device="cuda") for _ in range(2))
+    one, table = torch.ones(1, dtype=torch.int32, device="cuda"), torch.zeros(1, 4, dtype=torch.int32, device="cuda")
+    cu = torch.arange(2, dtype=torch.int32, device="cuda")
+    attend = lambda k, v, q: (lqer.lqer_kv4_append(pool, k, v, table[0, :1]), lqer.lqer_kv4_attention(pool, q, cu, one, table, 1, 1, 0.125))[1]  # noqa: E731
+    assert torch.equal(attend(odd(k), odd(v), odd(q)), attend(k, v, q))
