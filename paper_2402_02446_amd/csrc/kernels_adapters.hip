@@ -15,8 +15,8 @@
 // contiguous bytes of a row.  T goes into the second product as three bf16 terms (24 bits): X, A and B are bf16, so every product is
 // exact and the sums are fp32.
 //
-// Measured (projection + second product, us): 16 tokens of 4096 x 4096 rank 16 3.8 + 5.0; 64 of 8192 x 28672 with 48 adapters of up to 64 ranks
-// 7.5 + 24, B's lines at 5.3 TB/s; 203 of 4112 x 11000 5.0 + 7.1, sorting 3.6; 4096 of 8192 x 28672 rank 32 25 + 191, Y at 4.9 TB/s, sorting 8.
+// Measured (projection + second product, us): 16 tokens of 4096 x 4096 rank 16 3.8 + 5.1; 64 of 8192 x 28672 with 48 adapters of up to 64 ranks
+// 7.6 + 24, B's lines at 5.3 TB/s; 203 of 4112 x 11000 5.2 + 7.3, sorting 3.6; 4096 of 8192 x 28672 rank 32 26 + 192, Y at 4.9 TB/s, sorting 8.
 #include "serve.h"
 #include "mx_device.h"
 
@@ -513,7 +513,7 @@ size_t plan_adapters(AdapterArgs& a, void* workspace) {
     // Up to 64 tokens need no sorting.  Tiles of 16 tokens, whose four wavefronts share K, as long as they are not many; of 64, which read A and B a quarter
     // as often, beyond (us, 16 / 64: 300 tokens of 4096 x 4096 rank 16 14 / 17, 630 of 5696 x 2208 rank 64 23 / 31, 1000 of 672 x 532 rank 128
     // 18 / 30 and of 4096 x 4096 rank 16 21 / 22; 1000 of 4096 x 11008 rank 64 with 24 adapters 48 / 39, 1500 of 4096 x 4096 rank 32 27 / 25, 3000 of 2048 x 2048
-    // rank 128 56 / 44).
+    // rank 128 56 / 44).  By tokens alone the rule is wrong next to its limit for wide layers with many ranks, whose B counts: the 48 / 39.
     a.tile = a.M <= kWide ? 0 : a.M <= kNarrowTokens ? 16 : kWide;
     // Parts of K: at least 512 values each, at most 8 parts (that many loads sum T up at once), and with many tokens no more than give two
     // workgroups to a compute unit

@@ -8,11 +8,13 @@
 //   S^T = K Q^T      tokens as rows, query rows as columns: a lane holds half of the tokens of one row, the lane 32 further the others
 //   O^T += V^T P^T   the scores' registers are the operand as they are (tokens in the order in which the lanes hold them)
 // The running maximum is moved only when a score passes it by more than 2^8: until then the weights, relative to the older
-// maximum, are at most 2^8, which costs no precision, and the accumulators need no rescaling.  The weights enter the product as bf16
-// (relative 2^-8 at most), their sum in fp32.
+// maximum, are at most 2^8, which costs no precision, and the accumulators need no rescaling.  The weights enter the product as one bf16
+// term (relative 2^-8 at most), their sum in fp32: bf16 outputs are then 2.3e-3 from the exact ones (relative Frobenius; their own rounding is
+// 1.7e-3 of that).  Two terms take longer: 2 x 2048 queries on 6144 tokens, 64 / 8 heads, 718 us and with two terms 947, one prompt of 2048 92 and 114, 2 x 2048
+// queries on 6144 at D = 64 527 and 660, on 3008 at D = 256 262 and 294.
 //
-// Measured: 2 x 2048 queries on up to 6144 tokens, 64 / 8 heads of 128 (374 GFLOP) 400 to 460 us from card to card; the matrix instructions are busy
-// 38 % of the cycles, vector instructions 50 %, LDS 34 %: with two wavefronts to a SIMD they come one after another.  Not faster: reads
+// Measured: 2 x 2048 queries on up to 6144 tokens, 64 / 8 heads of 128 (374 GFLOP) 0.93 M cycles, which are 450 to 510 us in the first calls after a
+// pause and 400 after some sixty back to back, as the card's clock has it; the matrix instructions are busy 39 % of the cycles, vector instructions 51 %, LDS 35 %: with two wavefronts to a SIMD they come one after another.  Not faster: reads
 // of LDS scheduled ahead, exponentials pinned among the matrix instructions, wavefront priorities, tiles of 32 tokens with three workgroups
 // to a compute unit (13 % slower), 64 rows to a wavefront (35 % slower: 508 registers, one wavefront to a SIMD).
 #include "kv4_device.h"

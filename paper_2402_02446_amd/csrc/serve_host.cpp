@@ -14,7 +14,8 @@ constexpr int64_t kMaxGrid = 0x7FFFFFFF;
 // (a launch counts its threads in 32 bits: 256 to a tile of 64 tokens)
 constexpr int64_t kMaxAdapterTokens = 1 << 29;
 
-// The sizes of a call with adapters; false where it does not take them.  (N: the second axis of a grid counts 64 columns.)
+// The sizes of a call with adapters; false where it does not take them.  (N: the documented limit; blocks of 64 columns and workgroups for them are
+// counted in 32 bits, far from their end.)
 bool adapter_sizes(AdapterArgs& a, int64_t M, int64_t K, int64_t N, int R, int n) {
     if (M < 0 || M > kMaxAdapterTokens || K <= 0 || (K & 7) != 0 || N < 0 || N > 65535 * 64ll || R <= 0 || R > kMaxAdapterRank || (R & 7) != 0 || n <= 0 ||
         n > kMaxAdapters)
